@@ -228,6 +228,83 @@ int fasa_decode_step_paged(const fasa_shape* shape, const fasa_paging* paging, c
                            const int32_t* n_ctx_seq, const int32_t* budget_seq, float* S, int32_t* T,
                            float* O, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- chunks of new tokens, 8-bit caches -----------------------------------------------------------
+ * Around the decode step a serving program writes the rows of several new tokens at once (a prompt, a chunk of one,
+ * a few drafted tokens), attends over the cache from each of them, and may hold K and V in 8 bits.  The three calls
+ * below take the cache as a fasa_cache and the new tokens as a fasa_chunk; `paging` may be NULL: a contiguous cache,
+ * row (b, h, n) at b * kv_stride_b + h * kv_stride_h + n * kv_stride_n.
+ *
+ * 8-bit rows: one byte per value and one float32 scale per row (b, h, n), separately for K and V:
+ *     scale = max |x| / Q, rounded to float32, Q = 127 (FASA_CACHE_INT8) or 448 (FASA_CACHE_E4M3);
+ *     code  = the int8 (in [-127, 127]) or e4m3 (OCP 8-bit float: 4 exponent bits, 3 mantissa bits) number nearest to
+ *             x / scale, ties to even; 0 where scale is 0.  (max |x| below 2^-120: code is clamped to +-Q.)
+ * and the row stands for code * scale.  The quotient is rounded once, as if computed exactly, so codes do not depend on
+ * how a kernel divides.  A row with an infinity or a NaN gets the scale NaN and codes 0.
+ * Scales are laid out like the rows: scale of row (b, h, n) at b * scale_stride_b + h * scale_stride_h + n, or with
+ * paging at block * scale_stride_b + h * scale_stride_h + n % page_size.
+ * Alignment as above; 8-bit caches: kv strides multiples of 16 elements, scale strides multiples of 4. */
+typedef enum { FASA_CACHE_PLAIN = 0, FASA_CACHE_INT8 = 1, FASA_CACHE_E4M3 = 2 } fasa_cache_format;
+
+typedef struct fasa_cache {
+  void* K;                /* DEVICE: rows of shape->dtype (FASA_CACHE_PLAIN) or of bytes, strides kv_stride_{b,h,n} */
+  void* V;                /* in elements                                                                  */
+  float* k_scale;         /* DEVICE: scales of 8-bit rows; NULL for FASA_CACHE_PLAIN                       */
+  float* v_scale;
+  int64_t scale_stride_b; /* in floats; not used for FASA_CACHE_PLAIN                                      */
+  int64_t scale_stride_h;
+  int32_t format;         /* fasa_cache_format                                                            */
+  int32_t reserved;       /* must be 0                                                                    */
+} fasa_cache;
+
+/* The new tokens of a batch.  Sequence b has N_b tokens, the new ones counted, of which the last n_b are new: token i of
+ * them stands at position N_b - n_b + i of the sequence and in row  r = row_start[b] + i  (row_start == NULL:
+ * r = b * n_new + i) of q, k_new, v_new and O:
+ *     q + r * q_stride + hq * head_dim,  k_new / v_new + r * kv_stride + h * head_dim,  O + r * o_stride + hq * head_dim
+ * (so that for n_new == 1 the dense layouts are those of fasa_decode_step).  The arrays are read by the kernels when they run,
+ * as with fasa_decode_step_ragged: one call, or one captured graph of it, serves a growing ragged batch. */
+typedef struct fasa_chunk {
+  const int32_t* n_new_seq; /* DEVICE int32[batch] or NULL (n_new for all): n_b, clamped into [0, min(n_new, N_b)];
+                             * 0: the sequence takes no part                                              */
+  const int32_t* n_ctx_seq; /* DEVICE int32[batch] or NULL (shape->n_ctx for all): N_b, clamped into [0, shape->n_ctx] */
+  const int32_t* row_start; /* DEVICE int32[batch] or NULL: first row of each sequence, in any order; the sequences' rows may
+                             * not overlap.  Clamped into [0, n_rows], and n_b to the rows behind it        */
+  int64_t q_stride;         /* elements between rows of q, >= n_q_heads * head_dim, a multiple of 8          */
+  int64_t kv_stride;        /* of k_new and v_new, >= n_kv_heads * head_dim, a multiple of 8                 */
+  int64_t o_stride;         /* of O, like q_stride                                                         */
+  int32_t n_new;            /* most new tokens of a sequence, 1 .. shape->n_ctx                             */
+  int32_t n_rows;           /* rows that q, k_new, v_new and O have, with row_start; 0 without              */
+} fasa_chunk;
+
+/* Writes the rows of the new tokens (dtype) to their positions of the cache, K and V, in the cache's format.  Rows of no
+ * sequence are not read, rows of the cache at other positions and their scales are left as they were.  Two sequences may not write to
+ * one pool block's same row.  shape->budget and n_fc are not used, nor are q_stride and o_stride. */
+int fasa_cache_write(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const fasa_chunk* chunk,
+                     const void* k_new, const void* v_new, void* stream);
+
+/* Reads rows of the cache back in dtype (code * scale rounded once; a bit-exact copy for FASA_CACHE_PLAIN):
+ *     K_out, V_out [batch][n_kv_heads][n_end - n_begin][head_dim], either may be NULL;
+ *   T == NULL: tokens [n_begin, min(n_end, N_b)) of every sequence; what is beyond is left as it was;
+ *   else the rows that entries [n_begin, min(n_end, min(budget, N_b))) of T[b,h] name (row pitch of T: min(budget, n_ctx), as fasa_topk
+ *   writes it; entries are clamped into [0, N_b), and a sequence of no tokens gives none).
+ * n_ctx_seq: N_b as in fasa_chunk, or NULL.  0 <= n_begin <= n_end <= n_ctx (with T: <= min(budget, n_ctx)).
+ * What comes out is a contiguous cache of n_end - n_begin tokens for fasa_pack_kcache, fasa_dense_attend and the others. */
+int fasa_cache_read(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const int32_t* T,
+                    const int32_t* n_ctx_seq, int32_t n_begin, int32_t n_end, void* K_out, void* V_out, void* stream);
+
+/* Causal attention of the new tokens over the cache, which holds their own rows already (fasa_cache_write, or a decode step's
+ * append): for token i of sequence b, p = N_b - n_b + i, query head hq, h = hq / G
+ *     O[r,hq] = softmax_{n <= p}( q[r,hq] . K[b,h,n] / sqrt(d) ) V[b,h,n]
+ * q and O of dtype, float32 accumulation and softmax; bf16: the weights of a softmax go into the product with V as bf16 numbers
+ * (n_b * G > 16; up to that as two, 16 bits in all), O is rounded once.  8-bit rows enter as their codes, which bf16 holds
+ * exactly, and scales stay float32.  n_new == 1 is full-KV decode attention over a paged or 8-bit cache.
+ * Rows of O of no sequence are left as they were; rows of the cache at and beyond N_b and table entries beyond them have no effect,
+ * whatever they hold.  O may not overlap q.  budget and n_fc are not used.
+ * Needs a prepared workspace of fasa_chunk_workspace_bytes() (fasa_workspace_init, with any budget >= 1) and leaves it prepared; a
+ * workspace large enough serves the decode steps of the same batch and head counts too. */
+size_t fasa_chunk_workspace_bytes(const fasa_shape* shape, const fasa_chunk* chunk);
+int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const fasa_chunk* chunk,
+                      const void* q, void* O, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- memory-optimised variant (paper Sec. 4.3 and Alg. 2: "FASA-M") -----------------------------
  * Only the dominant key dims (Kp) stay on the device.  The non-dominant key dims and all values
  * live in PINNED HOST memory that the device can address (hipHostMalloc / a pinned torch tensor):

@@ -23,11 +23,13 @@ _LIB_PATH = os.environ.get("FASA_LIB") or os.path.join(os.path.dirname(os.path.a
 FASA_OK, FASA_EINVAL, FASA_EUNSUPPORTED, FASA_EWORKSPACE, FASA_EHIP = 0, -1, -2, -3, -4
 FASA_BF16, FASA_F32 = 0, 1
 FASA_PAIR_ROTATE_HALF, FASA_PAIR_INTERLEAVED, FASA_PAIR_LIST = 0, 1, 2
+FASA_CACHE_PLAIN, FASA_CACHE_INT8, FASA_CACHE_E4M3 = 0, 1, 2
 
 EXPORTS = [
     "fasa_workspace_bytes", "fasa_workspace_init", "fasa_validate_fc_idx", "fasa_pack_kcache", "fasa_score", "fasa_topk",
     "fasa_sparse_attend", "fasa_dense_attend", "fasa_decode_step", "fasa_decode_step_static", "fasa_decode_step_ragged",
     "fasa_pack_kcache_paged", "fasa_decode_step_paged",
+    "fasa_cache_write", "fasa_cache_read", "fasa_chunk_workspace_bytes", "fasa_chunk_attend",
     "fasa_offload_stage_bytes",
     "fasa_offload_split_kcache", "fasa_offload_decode_step", "fasa_calibration_workspace_bytes",
     "fasa_contextual_agreement", "fasa_select_dominant_fcs", "fasa_strerror",
@@ -48,6 +50,17 @@ class FasaShape(C.Structure):
 class FasaPaging(C.Structure):
     _fields_ = [("block_table", C.c_void_p), ("max_blocks", C.c_int32), ("page_size", C.c_int32),
                 ("n_pool_blocks", C.c_int32), ("reserved", C.c_int32)]
+
+
+class FasaCache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("scale_stride_b", C.c_int64), ("scale_stride_h", C.c_int64), ("format", C.c_int32), ("reserved", C.c_int32)]
+
+
+class FasaChunk(C.Structure):
+    _fields_ = [("n_new_seq", C.c_void_p), ("n_ctx_seq", C.c_void_p), ("row_start", C.c_void_p),
+                ("q_stride", C.c_int64), ("kv_stride", C.c_int64), ("o_stride", C.c_int64),
+                ("n_new", C.c_int32), ("n_rows", C.c_int32)]
 
 
 class FasaError(RuntimeError):
@@ -85,6 +98,11 @@ def _load():
     lib.fasa_pack_kcache_paged.restype = C.c_int
     lib.fasa_decode_step_paged.argtypes = [SP, PP, P, P, P, P, P, P, P, P, P, P, P, P, P, SZ, P]
     lib.fasa_decode_step_paged.restype = C.c_int
+    CP, HP = C.POINTER(FasaCache), C.POINTER(FasaChunk)
+    lib.fasa_cache_write.argtypes = [SP, PP, CP, HP, P, P, P]; lib.fasa_cache_write.restype = C.c_int
+    lib.fasa_cache_read.argtypes = [SP, PP, CP, P, P, I32, I32, P, P, P]; lib.fasa_cache_read.restype = C.c_int
+    lib.fasa_chunk_workspace_bytes.argtypes = [SP, HP]; lib.fasa_chunk_workspace_bytes.restype = SZ
+    lib.fasa_chunk_attend.argtypes = [SP, PP, CP, HP, P, P, P, SZ, P]; lib.fasa_chunk_attend.restype = C.c_int
     lib.fasa_offload_stage_bytes.argtypes = [SP]; lib.fasa_offload_stage_bytes.restype = SZ
     lib.fasa_offload_split_kcache.argtypes = [SP, P, P, P, P, I32, I32, P]
     lib.fasa_offload_split_kcache.restype = C.c_int
@@ -156,7 +174,8 @@ def _refuse(x, struct) -> None:
 
 
 def _bind(device) -> None:
-    _pycall.bind(_LIB_PATH, _ptr, device, torch._C._cuda_getCurrentRawStream, FasaShape, FasaPaging, _refuse)
+    _pycall.bind(_LIB_PATH, _ptr, device, torch._C._cuda_getCurrentRawStream, FasaShape, FasaPaging, _refuse,
+                 FasaCache, FasaChunk)
 
 
 def _first_device() -> int:
@@ -256,6 +275,46 @@ def fasa_decode_step_paged(shape, paging, q, K, V, Kp, fc_idx, k_new, v_new, n_c
                                    ws_bytes, stream)
     if rc:
         raise FasaError(rc, "fasa_decode_step_paged")
+
+
+def make_cache(K, V, format="plain", k_scale=None, v_scale=None, scale_stride_b=None, scale_stride_h=None) -> FasaCache:
+    """Cache struct (the tensors must outlive the calls).  format: FASA_CACHE_* or "plain" | "int8" | "e4m3".  Scale strides default to those of
+    the tensor k_scale [batch or blocks][n_kv_heads][tokens]."""
+    code = {"plain": FASA_CACHE_PLAIN, "int8": FASA_CACHE_INT8, "e4m3": FASA_CACHE_E4M3}.get(format, format)
+    if k_scale is not None:
+        scale_stride_b = k_scale.stride(0) if scale_stride_b is None else scale_stride_b
+        scale_stride_h = k_scale.stride(1) if scale_stride_h is None else scale_stride_h
+    return FasaCache(_ptr(K), _ptr(V), _ptr(k_scale), _ptr(v_scale), scale_stride_b or 0, scale_stride_h or 0, int(code), 0)
+
+
+def make_chunk(shape: FasaShape, n_new: int, n_new_seq=None, n_ctx_seq=None, row_start=None, n_rows: int = 0, q_stride=None,
+               kv_stride=None, o_stride=None) -> FasaChunk:
+    """Chunk struct (DEVICE int32 arrays, which must outlive the calls); rows default to dense [row][heads][head_dim]."""
+    q_row, kv_row = shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
+    return FasaChunk(_ptr(n_new_seq), _ptr(n_ctx_seq), _ptr(row_start), q_row if q_stride is None else q_stride,
+                     kv_row if kv_stride is None else kv_stride, q_row if o_stride is None else o_stride, n_new, n_rows)
+
+
+def fasa_cache_write(shape, paging, cache, chunk, k_new, v_new, stream=None) -> None:
+    rc = _pycall.cache_write(shape, paging, cache, chunk, k_new, v_new, stream)
+    if rc:
+        raise FasaError(rc, "fasa_cache_write")
+
+
+def fasa_cache_read(shape, paging, cache, T, n_ctx_seq, n_begin: int, n_end: int, K_out, V_out, stream=None) -> None:
+    rc = _pycall.cache_read(shape, paging, cache, T, n_ctx_seq, n_begin, n_end, K_out, V_out, stream)
+    if rc:
+        raise FasaError(rc, "fasa_cache_read")
+
+
+def fasa_chunk_workspace_bytes(shape: FasaShape, chunk: FasaChunk) -> int:
+    return int(_lib.fasa_chunk_workspace_bytes(C.byref(shape), C.byref(chunk)))
+
+
+def fasa_chunk_attend(shape, paging, cache, chunk, q, O, ws, ws_bytes: int, stream=None) -> None:
+    rc = _pycall.chunk_attend(shape, paging, cache, chunk, q, O, ws, ws_bytes, stream)
+    if rc:
+        raise FasaError(rc, "fasa_chunk_attend")
 
 
 def fasa_offload_stage_bytes(shape: FasaShape) -> int:

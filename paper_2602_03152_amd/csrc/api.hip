@@ -7,6 +7,7 @@
 #include <string>
 #include <vector>
 
+#include "chunk_common.h"
 #include "fasa_internal.h"
 
 namespace fasa {
@@ -466,6 +467,120 @@ int fasa_decode_step_paged(const fasa_shape* shape, const fasa_paging* paging, c
   if (!paging) return FASA_EINVAL;
   return decode_step_common(shape, paging, q, K, V, Kp, fc_idx, k_new, v_new, n_ctx_seq, budget_seq, S, T, O,
                             ws, ws_bytes, stream);
+}
+
+// ---- chunks of new tokens, 8-bit caches -----------------------------------------------------------
+namespace {
+int check_cache(const fasa_cache* c, const fasa_shape* s, const fasa_paging* paging, int n_reach, CacheView* out) {
+  if (!c || !c->K || !c->V || !aligned16(c->K) || !aligned16(c->V) || c->reserved != 0) return FASA_EINVAL;
+  if (c->format != FASA_CACHE_PLAIN && c->format != FASA_CACHE_INT8 && c->format != FASA_CACHE_E4M3) return FASA_EINVAL;
+  const bool bytes = c->format != FASA_CACHE_PLAIN;
+  if (bytes != (c->k_scale != nullptr) || bytes != (c->v_scale != nullptr)) return FASA_EINVAL;
+  if (bytes) {
+    if (!aligned16(c->k_scale) || !aligned16(c->v_scale)) return FASA_EINVAL;
+    if (s->kv_stride_n % 16 != 0 || s->kv_stride_h % 16 != 0 || s->kv_stride_b % 16 != 0) return FASA_EINVAL;
+    if (c->scale_stride_b < 0 || c->scale_stride_h < 0 || c->scale_stride_b % 4 != 0 || c->scale_stride_h % 4 != 0) return FASA_EINVAL;
+  }
+  PageMap pm = kNoPaging;
+  if (paging) {
+    fasa_shape cover = *s;
+    cover.n_ctx = n_reach;
+    const int rc = check_paging(paging, &cover, &pm);
+    if (rc != FASA_OK) return rc;
+  }
+  *out = CacheView{c->K, c->V, c->k_scale, c->v_scale, s->kv_stride_b, s->kv_stride_h, s->kv_stride_n, c->scale_stride_b, c->scale_stride_h, pm};
+  return FASA_OK;
+}
+
+constexpr unsigned kOfNew = 1, kOfQuery = 2;        // which rows of the chunk a call takes
+
+int check_chunk(const fasa_chunk* c, const fasa_shape* s, unsigned rows, ChunkView* out) {
+  if (!c || c->n_new < 1 || c->n_new > s->n_ctx) return FASA_EINVAL;
+  if (((uintptr_t)c->n_new_seq | (uintptr_t)c->n_ctx_seq | (uintptr_t)c->row_start) & 3u) return FASA_EINVAL;
+  if (c->row_start ? c->n_rows < 1 : c->n_rows != 0) return FASA_EINVAL;
+  const int64_t q_row = (int64_t)s->n_q_heads * s->head_dim, kv_row = (int64_t)s->n_kv_heads * s->head_dim;
+  if ((rows & kOfNew) && (c->kv_stride < kv_row || c->kv_stride % 8 != 0)) return FASA_EINVAL;
+  if ((rows & kOfQuery) && (c->q_stride < q_row || c->q_stride % 8 != 0 || c->o_stride < q_row || c->o_stride % 8 != 0)) return FASA_EINVAL;
+  // the kernels count rows times heads of a sequence, rows of the batch, and workgroups in 31 bits
+  if ((long long)c->n_new * s->n_q_heads > 0x7fffffffLL || (long long)s->batch * c->n_new > 0x7fffffffLL ||
+      (long long)c->n_rows * s->n_q_heads > 0x7fffffffLL || (long long)s->batch * c->n_new * s->n_q_heads > 8 * 0x7fffffffLL)
+    return FASA_EUNSUPPORTED;
+  *out = ChunkView{c->n_new_seq, c->n_ctx_seq, c->row_start, c->n_new, c->n_rows, s->n_ctx};
+  return FASA_OK;
+}
+
+struct ChunkLayout {
+  ChunkPlan plan;
+  size_t acc_off, ml_off, total;
+};
+// The part of the workspace that has to be zero comes first, where the other calls have it; the partial results behind it.
+ChunkLayout chunk_layout(fasa_shape s, const ChunkView& ch) {
+  ChunkLayout L;
+  L.plan = plan_chunk(s, ch.n_new, ch.n_rows, ch.row_start != nullptr);
+  s.budget = s.n_ctx;                     // (any: that part does not depend on it)
+  const WsLayout w = ws_layout(s);
+  L.acc_off = w.cand_off;
+  L.ml_off = align256(L.acc_off + L.plan.part_acc_bytes);
+  L.total = align256(L.ml_off + L.plan.part_ml_bytes);
+  return L;
+}
+}  // namespace
+
+int fasa_cache_write(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const fasa_chunk* chunk,
+                     const void* k_new, const void* v_new, void* stream) {
+  int rc = check_shape(shape, kNeedCtx | kNeedStrides);
+  if (rc != FASA_OK) return rc;
+  CacheView cv;
+  rc = check_cache(cache, shape, paging, shape->n_ctx, &cv);
+  if (rc != FASA_OK) return rc;
+  ChunkView ch;
+  rc = check_chunk(chunk, shape, kOfNew, &ch);
+  if (rc != FASA_OK) return rc;
+  if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return FASA_EINVAL;
+  FASA_HIP(launch_cache_write(*shape, cv, (CacheFmt)cache->format, ch, chunk->kv_stride, k_new, v_new, (hipStream_t)stream));
+  return FASA_OK;
+}
+
+int fasa_cache_read(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const int32_t* T,
+                    const int32_t* n_ctx_seq, int32_t n_begin, int32_t n_end, void* K_out, void* V_out, void* stream) {
+  int rc = check_shape(shape, kNeedCtx | kNeedStrides | (T ? (unsigned)kNeedBudget : 0u));
+  if (rc != FASA_OK) return rc;
+  CacheView cv;
+  rc = check_cache(cache, shape, paging, T ? shape->n_ctx : n_end, &cv);
+  if (rc != FASA_OK) return rc;
+  if ((!K_out && !V_out && n_begin != n_end) || !aligned16(K_out) || !aligned16(V_out) || ((uintptr_t)n_ctx_seq & 3u) || !aligned16(T)) return FASA_EINVAL;
+  const int most = T && shape->budget < shape->n_ctx ? shape->budget : shape->n_ctx;
+  if (n_begin < 0 || n_end < n_begin || n_end > most) return FASA_EINVAL;
+  if (n_begin == n_end) return FASA_OK;
+  FASA_HIP(launch_cache_read(*shape, cv, (CacheFmt)cache->format, T, n_ctx_seq, n_begin, n_end, K_out, V_out, (hipStream_t)stream));
+  return FASA_OK;
+}
+
+size_t fasa_chunk_workspace_bytes(const fasa_shape* shape, const fasa_chunk* chunk) {
+  ChunkView ch;
+  if (check_shape(shape, kNeedCtx | kNeedBudget) != FASA_OK || check_chunk(chunk, shape, 0, &ch) != FASA_OK) return 0;
+  // (fasa_workspace_init asks for as much as the other calls need)
+  return std::max(chunk_layout(*shape, ch).total, ws_layout(*shape).total);
+}
+
+int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const fasa_chunk* chunk,
+                      const void* q, void* O, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_shape(shape, kNeedCtx | kNeedStrides);
+  if (rc != FASA_OK) return rc;
+  CacheView cv;
+  rc = check_cache(cache, shape, paging, shape->n_ctx, &cv);
+  if (rc != FASA_OK) return rc;
+  ChunkView ch;
+  rc = check_chunk(chunk, shape, kOfQuery, &ch);
+  if (rc != FASA_OK) return rc;
+  if (!q || !O || !ws || !aligned16(q) || !aligned16(O) || !aligned16(ws)) return FASA_EINVAL;
+  const ChunkLayout L = chunk_layout(*shape, ch);
+  if (ws_bytes < L.total) return FASA_EWORKSPACE;
+  char* base = (char*)ws;
+  const ChunkArgs a{cv, ch, (CacheFmt)cache->format, q, O, chunk->q_stride, chunk->o_stride, (float*)(base + L.acc_off),
+                    (float*)(base + L.ml_off), (uint32_t*)base};
+  FASA_HIP(launch_chunk(*shape, L.plan, a, (hipStream_t)stream));
+  return FASA_OK;
 }
 
 size_t fasa_offload_stage_bytes(const fasa_shape* shape) {

@@ -1,0 +1,133 @@
+// Shared by the kernels around chunks of new tokens (cache.hip, chunk.hip, chunk_wide.hip): the cache and the chunk as the kernels see
+// them, and 8-bit values.
+#pragma once
+
+#include "attend_common.h"
+
+namespace fasa {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+enum CacheFmt { kPlain = FASA_CACHE_PLAIN, kInt8 = FASA_CACHE_INT8, kE4m3 = FASA_CACHE_E4M3 };
+
+// A cached row's storage: values of ET, or bytes.
+template <typename ET, CacheFmt F> struct RowType { using type = uint8_t; };
+template <typename ET> struct RowType<ET, kPlain> { using type = ET; };
+
+struct CacheView {
+  void *K, *V;
+  float *ks, *vs;               // null: rows of dtype
+  long long sb, sh, sn;         // elements between blocks (paged) or sequences, heads, tokens
+  long long ssb, ssh;           // of the scales
+  PageMap pm;
+};
+// block (or sequence) and token in it of token n of sequence b
+__device__ __forceinline__ void cache_place(const PageMap& pm, int b, int n, int& blk, int& off) {
+  if (pm.table == nullptr) { blk = b; off = n; return; }
+  blk = min(max(pm.table[(size_t)b * pm.max_blocks + (n >> pm.shift)], 0), pm.n_pool - 1);
+  off = n & ((1 << pm.shift) - 1);
+}
+
+struct ChunkView {
+  const int32_t *n_new_seq, *n_ctx_seq, *row_start;
+  int n_new, n_rows, n_ctx;
+};
+struct SeqChunk { int n_ctx, n_new, row; };      // a sequence's tokens, new tokens, first row
+__device__ __forceinline__ SeqChunk seq_chunk(const ChunkView& c, int b) {
+  SeqChunk s;
+  s.n_ctx = c.n_ctx_seq ? min(max(c.n_ctx_seq[b], 0), c.n_ctx) : c.n_ctx;
+  s.row = c.row_start ? min(max(c.row_start[b], 0), c.n_rows) : b * c.n_new;
+  int n = min(c.n_new_seq ? c.n_new_seq[b] : c.n_new, min(c.n_new, s.n_ctx));
+  if (c.row_start) n = min(n, c.n_rows - s.row);
+  s.n_new = max(n, 0);
+  return s;
+}
+
+// Work on a chunk goes by tiles of a sequence's items (rows, rows times heads).  Without row_start the rows of a sequence that
+// has fewer than n_new are padding that the caller has room for: every sequence gets the same number of tiles, and those behind its end have
+// nothing to do.  With row_start there may be many short sequences beside a long one, and batch * (tiles of the longest) of
+// workgroups would find nothing to do; there are n_rows in all, so n_rows * per_row / TILE + batch tiles are enough, and a
+// workgroup finds its own by counting them, 64 sequences at a time.  False: no tile left for it.
+template <int TILE>
+__device__ __forceinline__ bool find_chunk_tile(const ChunkView& c, int batch, int per_row, int tiles_each, unsigned id, int& b, int& tile) {
+  if (c.row_start == nullptr) {
+    b = (int)(id / (unsigned)tiles_each);
+    tile = (int)(id - (unsigned)b * tiles_each);
+    return b < batch;
+  }
+  uint32_t left = id;
+  for (int b0 = 0; b0 < batch; b0 += kWave) {
+    const int mine = b0 + lane_id();
+    const uint32_t v = mine < batch ? (uint32_t)(((long long)seq_chunk(c, mine).n_new * per_row + TILE - 1) / TILE) : 0u;
+    const uint32_t incl = wave_prefix_sum(v);
+    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
+    if (left < total) {
+      const int at = __builtin_ctzll(__ballot(incl > left));
+      b = b0 + at;
+      tile = (int)(left - (uint32_t)__builtin_amdgcn_readlane((int)(incl - v), at));
+      return true;
+    }
+    left -= total;
+  }
+  return false;
+}
+// tiles that the grid needs (an upper bound)
+inline long long chunk_tiles(bool by_row_start, int batch, int n_new, int n_rows, int per_row, int tile) {
+  return by_row_start ? (long long)n_rows * per_row / tile + batch : (long long)batch * (((long long)n_new * per_row + tile - 1) / tile);
+}
+
+// ---- 8-bit values ---------------------------------------------------------------------------------
+// Four bytes as two words of bf16 pairs.  Exact: an int8 has 8 significant bits, an e4m3 number 4.
+template <CacheFmt F> __device__ __forceinline__ uint2 bytes_to_bf16(uint32_t w) {
+  if constexpr (F == kE4m3) {
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)));
+  } else {
+    const float f0 = (float)(int8_t)w, f1 = (float)(int8_t)(w >> 8), f2 = (float)(int8_t)(w >> 16), f3 = (float)((int32_t)w >> 24);
+    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u),
+                      __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u));
+  }
+}
+template <CacheFmt F> __device__ __forceinline__ f32x4_t bytes_to_f32(uint32_t w) {
+  if constexpr (F == kE4m3) {
+    const uint2 p = bytes_to_bf16<F>(w);
+    return f32x4_t{bf16_lo(p.x), bf16_hi(p.x), bf16_lo(p.y), bf16_hi(p.y)};
+  } else {
+    return f32x4_t{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)((int32_t)w >> 24)};
+  }
+}
+// two float32 numbers as a word of bf16, to the nearest, ties to even
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const bf16x2_t r = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+// ---- launchers (shapes are validated) ----------------------------------------------------------------
+hipError_t launch_cache_write(const fasa_shape& s, const CacheView& cv, CacheFmt fmt, const ChunkView& ch, long long kv_stride, const void* k_new,
+                              const void* v_new, hipStream_t st);
+hipError_t launch_cache_read(const fasa_shape& s, const CacheView& cv, CacheFmt fmt, const int32_t* T, const int32_t* n_ctx_seq,
+                             int n_begin, int n_end, void* K_out, void* V_out, hipStream_t st);
+
+// How a chunk is attended.  wide: by chunk_wide.hip.  tiles: of the grid; per_seq: query tiles of the longest sequence; splits: of a tile's tokens.
+struct ChunkPlan {
+  bool wide;
+  int tile_rows;      // query rows (new token, head of the group) of a tile
+  int tiles, per_seq, splits;
+  size_t part_acc_bytes, part_ml_bytes;
+};
+ChunkPlan plan_chunk(const fasa_shape& s, int n_new, int n_rows, bool by_row_start);
+struct ChunkArgs {
+  CacheView cv;
+  ChunkView ch;
+  CacheFmt fmt;
+  const void* q;
+  void* O;
+  long long q_stride, o_stride;
+  float *part_acc, *part_ml;
+  uint32_t* tickets;            // [row][kChunkTickets], zero
+};
+constexpr int kChunkTickets = kHistBins;      // the words of a row's histogram, which are zero between calls
+hipError_t launch_chunk(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st);
+hipError_t launch_chunk_wide(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st);
+
+}  // namespace fasa

@@ -147,8 +147,11 @@ struct MfmaTile {
     for (int e = 0; e < 4; ++e) x[e] = valid[e] ? sv[e] : -INFINITY;   // weight exp2(-inf) = 0
     accumulate_full(kv, x, scs_wave, lo, hi);
   }
-  // a tile whose 16 rows all count (a logit of -inf: weight 0)
-  __device__ __forceinline__ void accumulate_full(const KV& kv, const float (&sv)[4], float* scs_wave, int lo, int hi) {
+  // a tile whose 16 rows all count (a logit of -inf: weight 0).  factor(e, w): what weight w of row 4hi + e enters the product with V as (the scale of
+  // an 8-bit row of V); the sum of the weights is without it.
+  struct AsItIs { __device__ float operator()(int, float w) const { return w; } };
+  template <class Factor = AsItIs>
+  __device__ __forceinline__ void accumulate_full(const KV& kv, const float (&sv)[4], float* scs_wave, int lo, int hi, Factor factor = Factor()) {
 #pragma clang fp contract(off)
     float mx = fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]));
     mx = xor32_max(xor16_max(mx));
@@ -162,6 +165,7 @@ struct MfmaTile {
     for (int e = 0; e < 4; ++e) {
       pv[e] = exp2_weight(sv[e] - m_new);
       psum += pv[e];
+      pv[e] = factor(e, pv[e]);
       ph[e] = __float_as_uint(pv[e]) & 0xffff0000u;
       pl[e] = __float_as_uint(pv[e] - __uint_as_float(ph[e]));   // exact; its own top 16 bits go in
     }

@@ -16,6 +16,7 @@ static PyObject *s_data_ptr, *s_cuda_stream; /* interned method and attribute na
 static PyObject *f_address;                  /* Python: address of anything else */
 static PyObject *f_device, *f_raw_stream;    /* torch._C: current device, its current stream */
 static PyObject *t_shape, *t_paging;         /* the binding's ctypes structures */
+static PyObject *t_cache, *t_chunk;
 static PyObject* f_refuse;                   /* Python: raises what ctypes raises for another object in their place */
 
 /* The conversions below leave *ok = 0 and an exception behind when they fail, and do nothing once that has
@@ -91,6 +92,9 @@ static int32_t int_of(PyObject* x, int* ok) { return (int32_t)int_bits(x, ok); }
 
 #define SHAPE(i) ((const fasa_shape*)structure(a[i], t_shape, &ok))
 #define PAGING(i) ((const fasa_paging*)structure(a[i], t_paging, &ok))
+#define PAGING_OR_NULL(i) (a[i] == Py_None ? NULL : PAGING(i))
+#define CACHE(i) ((const fasa_cache*)structure(a[i], t_cache, &ok))
+#define CHUNK(i) ((const fasa_chunk*)structure(a[i], t_chunk, &ok))
 #define P(i) address(a[i], &ok)
 #define I(i) int_of(a[i], &ok)
 #define Z(i) bytes_of(a[i], &ok)
@@ -142,12 +146,23 @@ ENTRY(offload_decode_step, 16, const fasa_shape* s = SHAPE(0); void* q = P(1); v
 ENTRY(contextual_agreement, 8, const fasa_shape* s = SHAPE(0); void* q = P(1); void* Kp = P(2); int32_t k = I(3);
       float* ca = P(4); void* ws = P(5); size_t z = Z(6); void* st = STREAM(7), s, q, Kp, k, ca, ws, z, st)
 
-/* bind(library path, address function, current device function, raw stream function, shape type, paging type, refusal) */
+ENTRY(cache_write, 7, const fasa_shape* s = SHAPE(0); const fasa_paging* pg = PAGING_OR_NULL(1); const fasa_cache* c = CACHE(2);
+      const fasa_chunk* ch = CHUNK(3); void* kn = P(4); void* vn = P(5); void* st = STREAM(6), s, pg, c, ch, kn, vn, st)
+ENTRY(cache_read, 10, const fasa_shape* s = SHAPE(0); const fasa_paging* pg = PAGING_OR_NULL(1); const fasa_cache* c = CACHE(2);
+      int32_t* T = P(3); int32_t* nc = P(4); int32_t n0 = I(5); int32_t n1 = I(6); void* K = P(7); void* V = P(8);
+      void* st = STREAM(9), s, pg, c, T, nc, n0, n1, K, V, st)
+ENTRY(chunk_attend, 9, const fasa_shape* s = SHAPE(0); const fasa_paging* pg = PAGING_OR_NULL(1); const fasa_cache* c = CACHE(2);
+      const fasa_chunk* ch = CHUNK(3); void* q = P(4); void* O = P(5); void* ws = P(6); size_t z = Z(7); void* st = STREAM(8),
+      s, pg, c, ch, q, O, ws, z, st)
+
+/* bind(library path, address function, current device function, raw stream function, shape type, paging type, refusal,
+ * cache type, chunk type) */
 static PyObject* py_bind(PyObject* self, PyObject* args) {
   (void)self;
   const char* path;
-  PyObject *adr, *dev, *raw, *shape, *paging, *refuse;
-  if (!PyArg_ParseTuple(args, "sOOOO!O!O", &path, &adr, &dev, &raw, &PyType_Type, &shape, &PyType_Type, &paging, &refuse))
+  PyObject *adr, *dev, *raw, *shape, *paging, *refuse, *cache, *chunk;
+  if (!PyArg_ParseTuple(args, "sOOOO!O!OO!O!", &path, &adr, &dev, &raw, &PyType_Type, &shape, &PyType_Type, &paging, &refuse,
+                        &PyType_Type, &cache, &PyType_Type, &chunk))
     return NULL;
   void* h = dlopen(path, RTLD_NOW); /* the copy that is loaded already */
   if (!h) { PyErr_SetString(PyExc_ImportError, dlerror()); return NULL; }
@@ -158,14 +173,17 @@ static PyObject* py_bind(PyObject* self, PyObject* args) {
   }
   BIND(pack_kcache) BIND(score) BIND(topk) BIND(sparse_attend) BIND(dense_attend) BIND(decode_step)
   BIND(decode_step_static) BIND(decode_step_ragged) BIND(pack_kcache_paged) BIND(decode_step_paged)
-  BIND(offload_decode_step) BIND(contextual_agreement)
+  BIND(offload_decode_step) BIND(contextual_agreement) BIND(cache_write) BIND(cache_read) BIND(chunk_attend)
   Py_INCREF(adr); Py_INCREF(dev); Py_INCREF(raw); Py_INCREF(shape); Py_INCREF(paging); Py_INCREF(refuse);
+  Py_INCREF(cache); Py_INCREF(chunk);
   Py_XSETREF(f_address, adr);
   Py_XSETREF(f_device, dev);
   Py_XSETREF(f_raw_stream, raw);
   Py_XSETREF(t_shape, shape);
   Py_XSETREF(t_paging, paging);
   Py_XSETREF(f_refuse, refuse);
+  Py_XSETREF(t_cache, cache);
+  Py_XSETREF(t_chunk, chunk);
   Py_RETURN_NONE;
 }
 
@@ -175,6 +193,7 @@ static PyMethodDef methods[] = {
     METHOD(pack_kcache), METHOD(score), METHOD(topk), METHOD(sparse_attend), METHOD(dense_attend),
     METHOD(decode_step), METHOD(decode_step_static), METHOD(decode_step_ragged), METHOD(pack_kcache_paged),
     METHOD(decode_step_paged), METHOD(offload_decode_step), METHOD(contextual_agreement),
+    METHOD(cache_write), METHOD(cache_read), METHOD(chunk_attend),
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
