@@ -42,7 +42,7 @@ PYCALL = os.path.join(PKG, "_pycall" + sysconfig.get_config_var("EXT_SUFFIX"))
 PYCALL_UNTAGGED = os.path.join(PKG, "_pycall.so")   # as it was once built: any interpreter would load it
 FLOORS = os.path.join(PKG, "fasa_floors")      # stand-alone measurement program (csrc/floors.hip)
 SOURCES = ["api.hip", "pack.hip", "score.hip", "topk.hip", "attend.hip", "fused.hip", "step.hip", "offload.hip", "calib.hip",
-           "cache.hip", "chunk.hip"]
+           "cache.hip", "chunk.hip", "chunk_wide.hip"]
 
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 FLAGS = [

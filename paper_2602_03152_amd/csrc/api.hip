@@ -579,7 +579,7 @@ int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const 
   char* base = (char*)ws;
   const ChunkArgs a{cv, ch, (CacheFmt)cache->format, q, O, chunk->q_stride, chunk->o_stride, (float*)(base + L.acc_off),
                     (float*)(base + L.ml_off), (uint32_t*)base};
-  FASA_HIP(launch_chunk(*shape, L.plan, a, (hipStream_t)stream));
+  FASA_HIP(L.plan.wide ? launch_chunk_wide(*shape, L.plan, a, (hipStream_t)stream) : launch_chunk(*shape, L.plan, a, (hipStream_t)stream));
   return FASA_OK;
 }
 

@@ -21,11 +21,16 @@ struct CacheView {
   long long ssb, ssh;           // of the scales
   PageMap pm;
 };
-// block (or sequence) and token in it of token n of sequence b
+// Block (without paging: sequence) and token in it of token n of sequence b.  In two steps, where the table is read ahead: the entry as it is, and
+// clamped into the pool.
+__device__ __forceinline__ int cache_block(const PageMap& pm, int b, int n) {
+  return pm.table ? pm.table[(size_t)b * pm.max_blocks + (n >> pm.shift)] : b;
+}
+__device__ __forceinline__ int cache_clamp(const PageMap& pm, int blk) { return pm.table ? min(max(blk, 0), pm.n_pool - 1) : blk; }
+__device__ __forceinline__ int cache_offset(const PageMap& pm, int n) { return pm.table ? n & ((1 << pm.shift) - 1) : n; }
 __device__ __forceinline__ void cache_place(const PageMap& pm, int b, int n, int& blk, int& off) {
-  if (pm.table == nullptr) { blk = b; off = n; return; }
-  blk = min(max(pm.table[(size_t)b * pm.max_blocks + (n >> pm.shift)], 0), pm.n_pool - 1);
-  off = n & ((1 << pm.shift) - 1);
+  blk = cache_clamp(pm, cache_block(pm, b, n));
+  off = cache_offset(pm, n);
 }
 
 struct ChunkView {
