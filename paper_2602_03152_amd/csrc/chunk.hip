@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int lo = lane & 15, hi = lane >> 4;
   const int pos0 = sc.n_ctx - sc.n_new;
-  const auto token_of = [&](int r) { return (qt * kChunkRows + r) / G; };
+  const auto token_of = [&](int r) FASA_INLINE { return (qt * kChunkRows + r) / G; };
   // tokens [0, seen) are seen by the last row of the tile
   const int seen = pos0 + token_of(rows - 1) + 1;
   const int share = ((seen + splits - 1) / splits + 15) & ~15;
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
   f32x4_t ks = {1.f, 1.f, 1.f, 1.f}, vs = ks;
   struct Place { long long k, v[4], vs[4]; } pl;       // rows and scales of the next tile
   // the tile's rows from token j0 on; tokens behind the split's last are the last again
-  auto find_rows = [&](int j0) {
+  auto find_rows = [&](int j0) FASA_INLINE {
     if constexpr (SMALL) {
       int blk, off;
       cache_place(cv.pm, b, min(j0 + lo, s1 - 1), blk, off);
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
       pl.vs[0] = sbase + min(4 * hi, last & ~3);                     // four at once: rows of scales are whole fours
     }
   };
-  auto load_k = [&]() {
+  auto load_k = [&]() FASA_INLINE {
     raw.load_k(Kh + pl.k);
     if constexpr (F != kPlain) {
       if constexpr (SMALL) {
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
       }
     }
   };
-  auto load_v = [&]() {
+  auto load_v = [&]() FASA_INLINE {
 #pragma unroll
     for (int e = 0; e < 4; ++e) raw.load_v(e, Vh + pl.v[e]);
     if constexpr (F != kPlain) {
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
   __syncthreads();
 
   // row r of the tile, to O
-  auto store_row = [&](int r, int d4, float4 a) {
+  auto store_row = [&](int r, int d4, float4 a) FASA_INLINE {
     const int tok = token_of(r);
     ET* o = O + (long long)(sc.row + tok) * o_stride + (long long)(h * G + (qt * kChunkRows + r) - tok * G) * D + 4 * d4;
     if constexpr (F32) *reinterpret_cast<float4*>(o) = a;

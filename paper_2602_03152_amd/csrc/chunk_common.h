@@ -8,6 +8,9 @@ namespace fasa {
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
+// for lambdas over register arrays: one that is called twice and not inlined has them in memory
+#define FASA_INLINE __attribute__((always_inline))
+
 enum CacheFmt { kPlain = FASA_CACHE_PLAIN, kInt8 = FASA_CACHE_INT8, kE4m3 = FASA_CACHE_E4M3 };
 
 // A cached row's storage: values of ET, or bytes.

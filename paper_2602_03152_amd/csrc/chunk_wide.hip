@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_wide_kernel(const uint16_t* 
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int pos0 = sc.n_ctx - sc.n_new;
-  const auto token_of = [&](int r) { return (qt * TR + r) / G; };
+  const auto token_of = [&](int r) FASA_INLINE { return (qt * TR + r) / G; };
   const int seen = pos0 + token_of(rows - 1) + 1;          // tokens that the tile's last row sees
   const int share = ((seen + splits - 1) / splits + kWideTok - 1) / kWideTok * kWideTok;
   const int s0 = min(split * share, seen), s1 = min(seen, s0 + share);
@@ -86,12 +86,12 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_wide_kernel(const uint16_t* 
   const RT* Vh = V + h * cv.sh;
   // A tile's blocks are looked up a tile ahead of its loads: a lookup between loads would wait for all loads before it.
   int blk[NL], sblk = 0;
-  auto look_up = [&](int j0) {
+  auto look_up = [&](int j0) FASA_INLINE {
 #pragma unroll
     for (int i = 0; i < NL; ++i) blk[i] = cache_block(cv.pm, b, min(j0 + (t + NT * i) / PER_ROW, s1 - 1));
     if constexpr (BYTES) sblk = cache_block(cv.pm, b, min(j0 + (t & 63), s1 - 1));
   };
-  auto load_tile = [&](int j0) {
+  auto load_tile = [&](int j0) FASA_INLINE {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int x = t + NT * i;
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_wide_kernel(const uint16_t* 
     }
     look_up(j0 + kWideTok);
   };
-  auto store_tile = [&](int buf) {
+  auto store_tile = [&](int buf) FASA_INLINE {
     unsigned char* k = smem + buf * 2 * kTileBytes;
     unsigned char* v = k + kTileBytes;
 #pragma unroll
@@ -245,6 +245,264 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_wide_kernel(const uint16_t* 
   if (half == 0) part_ml[at] = make_float2(m_run, l_run);
 }
 
+// The same for long chunks, eight waves of 32 queries (256 rows a tile), two a SIMD.  In steps of 32 tokens: step u runs the logits of step u + 1 and the
+// output of step u - 1 beside its own exponentials, in one block of straight code, so that the matrix cores have work while a wave is at its softmax.
+constexpr int kDeepWaves = 8, kDeepRows = 32 * kDeepWaves;
+constexpr int kDeepSlots = 3;                             // tiles of K, and of V, in LDS: K of tiles T, T + 1 and V of T - 1, T are read while K of T + 2 and V of T + 1 are written
+template <CacheFmt F>
+__global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const uint16_t* __restrict__ q, const typename RowType<uint16_t, F>::type* __restrict__ K,
+                                                            const typename RowType<uint16_t, F>::type* __restrict__ V, uint16_t* __restrict__ O,
+                                                            float* __restrict__ part_acc, float2* __restrict__ part_ml, CacheView cv, ChunkView ch,
+                                                            int batch, int Hkv, int G, int tiles_each, int splits, long long q_stride,
+                                                            long long o_stride, float scale_log2e) {
+  constexpr int D = kHeadDim, NT = 64 * kDeepWaves, TR = kDeepRows;
+  constexpr bool BYTES = F != kPlain;
+  using RT = typename RowType<uint16_t, F>::type;
+  constexpr int PER_ROW = BYTES ? 8 : 16;                 // 16-byte pieces of a stored row
+  constexpr int NL = kWideTok * PER_ROW / NT;             // pieces of K, and of V, a thread
+  constexpr int WROWS = 64 / PER_ROW;                     // rows of a wave's load
+  extern __shared__ __align__(16) unsigned char smem[];   // [slot] K tiles, [slot] V tiles, then scales [slot][k 64], [slot][v 64]
+  unsigned char* const smk = smem;
+  unsigned char* const smv = smem + kDeepSlots * kTileBytes;
+  float* const ssk = reinterpret_cast<float*>(smem + 2 * kDeepSlots * kTileBytes);
+  float* const ssv = ssk + kDeepSlots * kWideTok;
+
+  unsigned id = blockIdx.x;
+  const int h = (int)(id % (unsigned)Hkv);
+  id /= (unsigned)Hkv;
+  const int split = (int)(id % (unsigned)splits);
+  id /= (unsigned)splits;
+  int b, qt;
+  if (!find_chunk_tile<TR>(ch, batch, G, tiles_each, id, b, qt)) return;
+  const SeqChunk sc = seq_chunk(ch, b);
+  const int m = sc.n_new * G, m_tiles = (m + TR - 1) / TR;
+  if (qt >= m_tiles) return;
+  qt = m_tiles - 1 - qt;                                   // the longest first
+  const int rows = min(TR, m - qt * TR);
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int pos0 = sc.n_ctx - sc.n_new;
+  const auto token_of = [&](int r) FASA_INLINE { return (qt * TR + r) / G; };
+  const int seen = pos0 + token_of(rows - 1) + 1;          // tokens that the tile's last row sees
+  const int share = ((seen + splits - 1) / splits + kWideTok - 1) / kWideTok * kWideTok;
+  const int s0 = min(split * share, seen), s1 = min(seen, s0 + share);
+  const int n_tiles = (s1 - s0 + kWideTok - 1) / kWideTok;
+
+  // this lane's query
+  const int my = min(32 * wave + col, rows - 1), my_tok = token_of(my);
+  const int my_end = min(s1, pos0 + my_tok + 1);
+  const int wave_all = min(s1, pos0 + token_of(min(32 * wave, rows - 1)) + 1);         // tokens that all of the wave's queries see
+  bf16x8_t qb[8];
+  {
+    const uint16_t* p = q + (long long)(sc.row + my_tok) * q_stride + (long long)(h * G + (qt * TR + my) - my_tok * G) * D + 8 * half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) qb[i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(p + 16 * i));
+  }
+  f32x16_t oc[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) oc[i] = f32x16_t{};
+  float m_run = kNegBig, l_run = 0.f;
+
+  // ---- loader ----
+  // A wave's load is WROWS rows, which lie in one block (pages of that many tokens or more): where they begin is the wave's, in scalar registers; what is
+  // a lane's is its row and piece in there, clamped to the last row that there is.  Lane l looks up the block of a tile's token l a tile ahead.
+  const bool paged = cv.pm.table != nullptr;
+  const int32_t* const table = paged ? cv.pm.table + (size_t)b * cv.pm.max_blocks : reinterpret_cast<const int32_t*>(q);
+  const int shift = paged ? cv.pm.shift : 31, in_block = paged ? (1 << cv.pm.shift) - 1 : 0x7fffffff;
+  const int blk_min = paged ? 0 : b, blk_max = paged ? cv.pm.n_pool - 1 : b;
+  const uint32_t row_bytes = (uint32_t)cv.sn * (uint32_t)sizeof(RT);
+  const uint32_t my_row = (uint32_t)(lane / PER_ROW) * row_bytes, my_piece = (uint32_t)(lane % PER_ROW) * 16;
+  const char* const Kh = reinterpret_cast<const char*>(K + h * cv.sh);
+  const char* const Vh = reinterpret_cast<const char*>(V + h * cv.sh);
+  typedef uint32_t u32xl __attribute__((ext_vector_type(4 * NL)));
+  auto look_up = [&](int j0) FASA_INLINE { return table[min(j0 + lane, s1 - 1) >> shift]; };
+  auto load_rows = [&](const char* H, int j0, int blks) FASA_INLINE {
+    u32xl r;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int g = min(j0 + WROWS * (wave + kDeepWaves * i), (s1 - 1) & ~(WROWS - 1));
+      const int blk = min(max(__builtin_amdgcn_readlane(blks, max(g - j0, 0)), blk_min), blk_max);
+      const char* base = H + (blk * cv.sb + (g & in_block) * cv.sn) * (long long)sizeof(RT);
+      const uint32_t off = min(my_row, (uint32_t)min(s1 - 1 - g, WROWS - 1) * row_bytes) + my_piece;
+      const uint4 x = *reinterpret_cast<const uint4*>(base + off);
+      r[4 * i] = x.x; r[4 * i + 1] = x.y; r[4 * i + 2] = x.z; r[4 * i + 3] = x.w;
+    }
+    return r;
+  };
+  auto load_scale = [&](const float* s, int j0, int blks) FASA_INLINE {
+    return s[min(max(blks, blk_min), blk_max) * cv.ssb + h * cv.ssh + (min(j0 + lane, s1 - 1) & in_block)];
+  };
+  auto store_rows = [&](unsigned char* to, u32xl r, auto swz) FASA_INLINE {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = WROWS * (wave + kDeepWaves * i) + lane / PER_ROW, c = lane % PER_ROW;
+      if constexpr (BYTES) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint2 lo = bytes_to_bf16<F>(r[4 * i + 2 * j]), hi = bytes_to_bf16<F>(r[4 * i + 2 * j + 1]);
+          *reinterpret_cast<uint4*>(to + row * 256 + (((2 * c + j) ^ swz(row)) << 4)) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
+      } else {
+        *reinterpret_cast<uint4*>(to + row * 256 + ((c ^ swz(row)) << 4)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+      }
+    }
+  };
+
+  // ---- products ----
+  uint32_t k_at[8], v_at[4];                               // places of this lane's operands in a tile, of its first 32 (16) tokens
+#pragma unroll
+  for (int s = 0; s < 8; ++s) k_at[s] = col * 256 + (((2 * s + half) ^ swz_k(col)) << 4);
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int r = 4 * half + ((lane & 15) >> 2), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    v_at[d] = r * 256 + ((c ^ swz_v(r)) << 4) + 8 * (lane & 1);
+  }
+  struct Weights { uint32_t w[8]; };
+  auto logits = [&](const unsigned char* kt, f32x16_t& sv) FASA_INLINE {
+    sv = f32x16_t{};
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      sv = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(kt + k_at[s])), qb[s], sv, 0, 0, 0);
+  };
+  auto output = [&](const unsigned char* vt, const Weights& p) FASA_INLINE {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const unsigned char* at = vt + v_at[d] + s * 16 * 256;
+        const uint2 lo = lds_read_tr(at), hi = lds_read_tr(at + 8 * 256);                // (rows r and r + 8 have the same swizzle)
+        oc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)),
+                                                        __builtin_bit_cast(bf16x8_t, make_uint4(p.w[4 * s], p.w[4 * s + 1], p.w[4 * s + 2], p.w[4 * s + 3])), oc[d], 0, 0, 0);
+      }
+  };
+  auto by_scale = [&](f32x16_t& sv, const float* f) FASA_INLINE {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float4 x = *reinterpret_cast<const float4*>(f + 8 * g + 4 * half);
+      sv[4 * g] *= x.x; sv[4 * g + 1] *= x.y; sv[4 * g + 2] *= x.z; sv[4 * g + 3] *= x.w;
+    }
+  };
+  // Weights of logits sv (tokens n0 .. n0 + 31); by: the factor by which the running sums go down.
+  auto softmax = [&](f32x16_t& sv, Weights& p, float& by, int n0, const float* ks, const float* vs, auto masked) FASA_INLINE {
+    if constexpr (BYTES) by_scale(sv, ks);
+    if constexpr (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sv[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < my_end ? sv[i] : -INFINITY;
+    }
+    float mx = fmaxf(sv[0], sv[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) mx = fmaxf(mx, fmaxf(sv[i], sv[i + 1]));
+    mx = xor32_max(mx);
+    if constexpr (!BYTES) mx *= scale_log2e;
+    const float m_new = fmaxf(m_run, mx);
+    by = __builtin_amdgcn_exp2f(m_run - m_new);
+    m_run = m_new;
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sv[i] = __builtin_amdgcn_exp2f(BYTES ? sv[i] - m_new : __builtin_fmaf(sv[i], scale_log2e, -m_new));
+      sum[i & 1] += sv[i];
+    }
+    l_run = __builtin_fmaf(l_run, by, sum[0] + sum[1]);
+    if constexpr (BYTES) by_scale(sv, vs);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p.w[i] = pack_bf16(sv[2 * i], sv[2 * i + 1]);
+  };
+  // step: logits of the next 32 tokens -> nxt, output of the ones before (pp), weights of these (cur -> pc)
+  auto step = [&](f32x16_t& cur, f32x16_t& nxt, const Weights& pp, Weights& pc, const unsigned char* k_next, const unsigned char* v_last, int n0, const float* ks,
+                  const float* vs, auto masked) FASA_INLINE {
+    float by;
+    logits(k_next, nxt);
+    output(v_last, pp);
+    softmax(cur, pc, by, n0, ks, vs, masked);
+#ifdef FASA_SGB
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+#endif
+    if (__ballot(by != 1.f) != 0ull) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) oc[d] *= by;
+    }
+  };
+
+  if (n_tiles > 0) {
+    f32x16_t sa, sb;
+    Weights pa = {}, pb;
+    const auto of_k = [](int r) { return swz_k(r); };
+    const auto of_v = [](int r) { return swz_v(r); };
+    float rsk = 0.f, rsv = 0.f;
+    // K of tiles 0 and 1, V of tile 0; zeros for V of the tile before the first, which has no weights, but what 0 is multiplied by has to be a number
+    int blk0 = look_up(s0), blk1 = look_up(s0 + kWideTok), blk2 = look_up(s0 + 2 * kWideTok);
+    store_rows(smk, load_rows(Kh, s0, blk0), of_k);
+    store_rows(smv, load_rows(Vh, s0, blk0), of_v);
+    store_rows(smk + kTileBytes, load_rows(Kh, s0 + kWideTok, blk1), of_k);
+    if constexpr (BYTES) {
+      ssk[lane] = load_scale(cv.ks, s0, blk0) * scale_log2e;                            // (all waves, the same)
+      ssv[lane] = load_scale(cv.vs, s0, blk0);
+      ssk[kWideTok + lane] = load_scale(cv.ks, s0 + kWideTok, blk1) * scale_log2e;
+      rsk = load_scale(cv.ks, s0 + 2 * kWideTok, blk2);
+    }
+    for (int x = t; x < kTileBytes / 16; x += NT) reinterpret_cast<uint4*>(smv + (kDeepSlots - 1) * kTileBytes)[x] = make_uint4(0, 0, 0, 0);
+    u32xl raw = load_rows(Kh, s0 + 2 * kWideTok, blk2);
+    int blk3 = look_up(s0 + 3 * kWideTok);
+    __syncthreads();
+    logits(smk, sa);
+    int c0 = 0, c1 = 1, c2 = 2;                            // slots of tiles T, T + 1, T + 2 (= T - 1)
+    const int n_plain = max(0, min(n_tiles, (wave_all - s0) / kWideTok));   // tiles without a mask
+    // before tile T: raw is K of tile T + 2; blk1 .. blk3: blocks of tiles T + 1 .. T + 3
+    auto tile = [&](int T, auto masked) FASA_INLINE {
+      const int j0 = s0 + T * kWideTok;
+      store_rows(smk + c2 * kTileBytes, raw, of_k);
+      raw = load_rows(Vh, j0 + kWideTok, blk1);
+      if constexpr (BYTES) {
+        ssk[c2 * kWideTok + lane] = rsk * scale_log2e;
+        rsv = load_scale(cv.vs, j0 + kWideTok, blk1);
+      }
+      step(sa, sb, pa, pb, smk + c0 * kTileBytes + 32 * 256, smv + c2 * kTileBytes + 32 * 256, j0, ssk + c0 * kWideTok, ssv + c0 * kWideTok, masked);
+      store_rows(smv + c1 * kTileBytes, raw, of_v);
+      raw = load_rows(Kh, j0 + 3 * kWideTok, blk3);
+      if constexpr (BYTES) {
+        ssv[c1 * kWideTok + lane] = rsv;
+        rsk = load_scale(cv.ks, j0 + 3 * kWideTok, blk3);
+      }
+      blk1 = blk2; blk2 = blk3;
+      blk3 = look_up(j0 + 4 * kWideTok);
+      step(sb, sa, pb, pa, smk + c1 * kTileBytes, smv + c0 * kTileBytes, j0 + 32, ssk + c0 * kWideTok + 32, ssv + c0 * kWideTok + 32, masked);
+      __syncthreads();
+      const int c = c0; c0 = c1; c1 = c2; c2 = c;
+    };
+    // every wave runs all tiles, for the barriers
+    for (int T = 0; T < n_plain; ++T) tile(T, std::false_type{});
+    for (int T = n_plain; T < n_tiles; ++T) tile(T, std::true_type{});
+    output(smv + c2 * kTileBytes + 32 * 256, pa);
+  }
+  l_run = xor32_sum(l_run);
+  if (32 * wave + col >= rows) return;
+  if (splits == 1) {
+    const float by = 1.0f / l_run;
+    uint16_t* o = O + (long long)(sc.row + my_tok) * o_stride + (long long)(h * G + (qt * TR + my) - my_tok * G) * D + 4 * half;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<uint2*>(o + 32 * d + 8 * g) = make_uint2(pack_bf16(oc[d][4 * g] * by, oc[d][4 * g + 1] * by), pack_bf16(oc[d][4 * g + 2] * by, oc[d][4 * g + 3] * by));
+    return;
+  }
+  const size_t at = (((size_t)(b * Hkv + h) * tiles_each + qt) * splits + split) * TR + my;
+  float* to = part_acc + at * D + 4 * half;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<float4*>(to + 32 * d + 8 * g) = make_float4(oc[d][4 * g], oc[d][4 * g + 1], oc[d][4 * g + 2], oc[d][4 * g + 3]);
+  if (half == 0) part_ml[at] = make_float2(m_run, l_run);
+}
+
 // Joins the splits of a tile's rows: 32 lanes a row, four dims each.
 template <int TR>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restrict__ part_acc, const float2* __restrict__ part_ml, uint16_t* __restrict__ O,
@@ -287,10 +545,25 @@ static hipError_t wide_t(const fasa_shape& s, const ChunkPlan& p, const ChunkArg
                 (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.o_stride);
 }
 
+template <CacheFmt F> static hipError_t deep_t(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
+  using RT = typename RowType<uint16_t, F>::type;
+  const int hkv = s.n_kv_heads, G = s.n_q_heads / hkv;
+  const hipError_t e = launch_lds("fasa_chunk_attend", chunk_deep_kernel<F>, dim3((unsigned)((long long)p.tiles * hkv * p.splits)), dim3(64 * kDeepWaves),
+                                  2 * kDeepSlots * (kTileBytes + (F == kPlain ? 0 : kWideTok * 4)), st, (const uint16_t*)a.q, (const RT*)a.cv.K, (const RT*)a.cv.V,
+                                  (uint16_t*)a.O, a.part_acc, (float2*)a.part_ml, a.cv, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.q_stride, a.o_stride,
+                                  1.4426950408889634f / sqrtf((float)s.head_dim));
+  if (e != hipSuccess || p.splits == 1) return e;
+  return launch("fasa_chunk_merge", chunk_merge_kernel<kDeepRows>, dim3((unsigned)p.tiles * (kDeepRows / 8), hkv), dim3(256), st, (const float*)a.part_acc,
+                (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.o_stride);
+}
+
 hipError_t launch_chunk_wide(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
   if (p.tile_rows == 128)
     return a.fmt == kPlain ? wide_t<kPlain, 4>(s, p, a, st) : a.fmt == kInt8 ? wide_t<kInt8, 4>(s, p, a, st) : wide_t<kE4m3, 4>(s, p, a, st);
-  return a.fmt == kPlain ? wide_t<kPlain, 8>(s, p, a, st) : a.fmt == kInt8 ? wide_t<kInt8, 8>(s, p, a, st) : wide_t<kE4m3, 8>(s, p, a, st);
+  // pages of fewer tokens than a wave's load has rows, or rows far apart: tokens are looked up one by one
+  const bool apart = (a.cv.pm.table != nullptr && (1 << a.cv.pm.shift) < (a.fmt == kPlain ? 4 : 8)) || a.cv.sn >= (1ll << 28);
+  if (apart) return a.fmt == kPlain ? wide_t<kPlain, 8>(s, p, a, st) : a.fmt == kInt8 ? wide_t<kInt8, 8>(s, p, a, st) : wide_t<kE4m3, 8>(s, p, a, st);
+  return a.fmt == kPlain ? deep_t<kPlain>(s, p, a, st) : a.fmt == kInt8 ? deep_t<kInt8>(s, p, a, st) : deep_t<kE4m3>(s, p, a, st);
 }
 
 }  // namespace fasa
