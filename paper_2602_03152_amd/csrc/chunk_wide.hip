@@ -23,7 +23,7 @@ __device__ __forceinline__ int swz_k(int t) { return t & 15; }
 __device__ __forceinline__ int swz_v(int t) { return 2 * (t & 7); }
 
 // Four bf16 of one column of V for each of 16 lanes, out of four rows of LDS
-__device__ __forceinline__ uint2 lds_read_tr(const unsigned char* p) {
+__device__ __forceinline__ uint2 lds_read_tr(__attribute__((address_space(3))) const unsigned char* p) {
   const s16x4_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)p);
   return __builtin_bit_cast(uint2, r);
 }
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_wide_kernel(const uint16_t* 
           const int r = 16 * s + 4 * half + ((lane & 15) >> 2), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
           const unsigned char* at = vt + ((c ^ swz_v(r)) << 4) + 8 * (lane & 1) + r * 256;
           const unsigned char* at8 = vt + ((c ^ swz_v(r + 8)) << 4) + 8 * (lane & 1) + (r + 8) * 256;
-          const uint2 lo = lds_read_tr(at), hi = lds_read_tr(at8);
+          const uint2 lo = lds_read_tr((__attribute__((address_space(3))) const unsigned char*)at), hi = lds_read_tr((__attribute__((address_space(3))) const unsigned char*)at8);
           oc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), p, oc[d], 0, 0, 0);
         }
       }
@@ -243,6 +243,14 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_wide_kernel(const uint16_t* 
     for (int g = 0; g < 4; ++g)
       *reinterpret_cast<float4*>(pa + 32 * d + 8 * g) = make_float4(oc[d][4 * g], oc[d][4 * g + 1], oc[d][4 * g + 2], oc[d][4 * g + 3]);
   if (half == 0) part_ml[at] = make_float2(m_run, l_run);
+}
+
+// largest of a lane's sixteen logits
+__device__ __forceinline__ float largest(const f32x16_t& v) {
+  float m = __builtin_fmaxf(v[0], v[1]);
+#pragma unroll
+  for (int i = 2; i < 16; i += 2) m = __builtin_fmaxf(m, __builtin_fmaxf(v[i], v[i + 1]));
+  return m;
 }
 
 // The same for long chunks, eight waves of 32 queries (256 rows a tile), two a SIMD.  In steps of 32 tokens: step u runs the logits of step u + 1 and the
@@ -304,33 +312,45 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
   float m_run = kNegBig, l_run = 0.f;
 
   // ---- loader ----
-  // A wave's load is WROWS rows, which lie in one block (pages of that many tokens or more): where they begin is the wave's, in scalar registers; what is
-  // a lane's is its row and piece in there, clamped to the last row that there is.  Lane l looks up the block of a tile's token l a tile ahead.
+  // A wave's load is WROWS rows, which lie in one block (pages of that many tokens or more): where they begin is the wave's, in scalar registers, and the same for
+  // K and V; what is a lane's is its row and piece in there, clamped to the last row that there is.  Lane l looks up the block of a tile's token l.
   const bool paged = cv.pm.table != nullptr;
   const int32_t* const table = paged ? cv.pm.table + (size_t)b * cv.pm.max_blocks : reinterpret_cast<const int32_t*>(q);
   const int shift = paged ? cv.pm.shift : 31, in_block = paged ? (1 << cv.pm.shift) - 1 : 0x7fffffff;
-  const int blk_min = paged ? 0 : b, blk_max = paged ? cv.pm.n_pool - 1 : b;
-  const uint32_t row_bytes = (uint32_t)cv.sn * (uint32_t)sizeof(RT);
+  const int blk_max = paged ? cv.pm.n_pool - 1 : 0;
+  const uint32_t blk_bytes = paged ? (uint32_t)(cv.sb * (int)sizeof(RT)) : 0, row_bytes = (uint32_t)(cv.sn * (int)sizeof(RT));
+  const long long seq = (paged ? 0 : b * cv.sb) + h * cv.sh;
+  const char* const Kh = reinterpret_cast<const char*>(K + seq);
+  const char* const Vh = reinterpret_cast<const char*>(V + seq);
   const uint32_t my_row = (uint32_t)(lane / PER_ROW) * row_bytes, my_piece = (uint32_t)(lane % PER_ROW) * 16;
-  const char* const Kh = reinterpret_cast<const char*>(K + h * cv.sh);
-  const char* const Vh = reinterpret_cast<const char*>(V + h * cv.sh);
   typedef uint32_t u32xl __attribute__((ext_vector_type(4 * NL)));
+  struct Rows { uint64_t at[NL]; uint32_t last[NL]; int blk; };     // of a tile: where this wave's loads begin, bytes to the last row of them; lane l: block of token l
   auto look_up = [&](int j0) FASA_INLINE { return table[min(j0 + lane, s1 - 1) >> shift]; };
-  auto load_rows = [&](const char* H, int j0, int blks) FASA_INLINE {
-    u32xl r;
+  auto rows_of = [&](int j0, int blks) FASA_INLINE {
+    Rows r;
+    r.blk = min(max(blks, 0), blk_max);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int g = min(j0 + WROWS * (wave + kDeepWaves * i), (s1 - 1) & ~(WROWS - 1));
-      const int blk = min(max(__builtin_amdgcn_readlane(blks, max(g - j0, 0)), blk_min), blk_max);
-      const char* base = H + (blk * cv.sb + (g & in_block) * cv.sn) * (long long)sizeof(RT);
-      const uint32_t off = min(my_row, (uint32_t)min(s1 - 1 - g, WROWS - 1) * row_bytes) + my_piece;
-      const uint4 x = *reinterpret_cast<const uint4*>(base + off);
-      r[4 * i] = x.x; r[4 * i + 1] = x.y; r[4 * i + 2] = x.z; r[4 * i + 3] = x.w;
+      const uint32_t blk = (uint32_t)__builtin_amdgcn_readlane(r.blk, max(g - j0, 0));
+      r.at[i] = (uint64_t)blk * blk_bytes + (uint64_t)(uint32_t)(g & in_block) * row_bytes;
+      r.last[i] = (uint32_t)min(s1 - 1 - g, WROWS - 1) * row_bytes;
     }
     return r;
   };
-  auto load_scale = [&](const float* s, int j0, int blks) FASA_INLINE {
-    return s[min(max(blks, blk_min), blk_max) * cv.ssb + h * cv.ssh + (min(j0 + lane, s1 - 1) & in_block)];
+  auto load_rows = [&](const char* H, const Rows& r) FASA_INLINE {
+    u32xl v;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const uint4 x = *reinterpret_cast<const uint4*>(H + r.at[i] + (min(my_row, r.last[i]) + my_piece));
+      v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+    }
+    return v;
+  };
+  const float* const ks_h = BYTES ? cv.ks + (paged ? 0 : b * cv.ssb) + h * cv.ssh : nullptr;
+  const float* const vs_h = BYTES ? cv.vs + (paged ? 0 : b * cv.ssb) + h * cv.ssh : nullptr;
+  auto load_scale = [&](const float* s, int j0, const Rows& r) FASA_INLINE {
+    return s[r.blk * (paged ? cv.ssb : 0) + (min(j0 + lane, s1 - 1) & in_block)];
   };
   auto store_rows = [&](unsigned char* to, u32xl r, auto swz) FASA_INLINE {
 #pragma unroll
@@ -349,28 +369,29 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
   };
 
   // ---- products ----
-  uint32_t k_at[8], v_at[4];                               // places of this lane's operands in a tile, of its first 32 (16) tokens
+  typedef __attribute__((address_space(3))) const unsigned char* lds_ptr;
+  lds_ptr k_at[8], v_at[4];                                // places of this lane's operands in slot 0, of its first 32 (16) tokens
 #pragma unroll
-  for (int s = 0; s < 8; ++s) k_at[s] = col * 256 + (((2 * s + half) ^ swz_k(col)) << 4);
+  for (int s = 0; s < 8; ++s) k_at[s] = (lds_ptr)smk + col * 256 + (((2 * s + half) ^ swz_k(col)) << 4);
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
     const int r = 4 * half + ((lane & 15) >> 2), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    v_at[d] = r * 256 + ((c ^ swz_v(r)) << 4) + 8 * (lane & 1);
+    v_at[d] = (lds_ptr)smv + r * 256 + ((c ^ swz_v(r)) << 4) + 8 * (lane & 1);
   }
   struct Weights { uint32_t w[8]; };
-  auto logits = [&](const unsigned char* kt, f32x16_t& sv) FASA_INLINE {
-    sv = f32x16_t{};
+  // at: where the 32 tokens begin, in bytes from slot 0
+  auto logits = [&](int at, f32x16_t& sv) FASA_INLINE {
 #pragma unroll
     for (int s = 0; s < 8; ++s)
-      sv = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(kt + k_at[s])), qb[s], sv, 0, 0, 0);
+      sv = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t*)(k_at[s] + at)), qb[s], s == 0 ? f32x16_t{} : sv, 0, 0, 0);
   };
-  auto output = [&](const unsigned char* vt, const Weights& p) FASA_INLINE {
+  auto output = [&](int at, const Weights& p) FASA_INLINE {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const unsigned char* at = vt + v_at[d] + s * 16 * 256;
-        const uint2 lo = lds_read_tr(at), hi = lds_read_tr(at + 8 * 256);                // (rows r and r + 8 have the same swizzle)
+        const lds_ptr from = v_at[d] + (at + s * 16 * 256);
+        const uint2 lo = lds_read_tr(from), hi = lds_read_tr(from + 8 * 256);            // (rows r and r + 8 have the same swizzle)
         oc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)),
                                                         __builtin_bit_cast(bf16x8_t, make_uint4(p.w[4 * s], p.w[4 * s + 1], p.w[4 * s + 2], p.w[4 * s + 3])), oc[d], 0, 0, 0);
       }
@@ -383,47 +404,46 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
     }
   };
   // Weights of logits sv (tokens n0 .. n0 + 31); by: the factor by which the running sums go down.
-  auto softmax = [&](f32x16_t& sv, Weights& p, float& by, int n0, const float* ks, const float* vs, auto masked) FASA_INLINE {
+  auto softmax = [&](f32x16_t& sv, Weights& p, float& by, int n0, const float* ks, const float* vs) FASA_INLINE {
     if constexpr (BYTES) by_scale(sv, ks);
-    if constexpr (masked) {
+    if (n0 + 32 > wave_all) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sv[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < my_end ? sv[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) sv[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < my_end ? sv[i] : kNegBig;
     }
-    float mx = fmaxf(sv[0], sv[1]);
-#pragma unroll
-    for (int i = 2; i < 16; i += 2) mx = fmaxf(mx, fmaxf(sv[i], sv[i + 1]));
-    mx = xor32_max(mx);
+    float mx = xor32_max(largest(sv));
     if constexpr (!BYTES) mx *= scale_log2e;
     const float m_new = fmaxf(m_run, mx);
     by = __builtin_amdgcn_exp2f(m_run - m_new);
     m_run = m_new;
-    float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      sv[i] = __builtin_amdgcn_exp2f(BYTES ? sv[i] - m_new : __builtin_fmaf(sv[i], scale_log2e, -m_new));
-      sum[i & 1] += sv[i];
+    for (int i = 0; i < 16; ++i) sv[i] = __builtin_amdgcn_exp2f(BYTES ? sv[i] - m_new : __builtin_fmaf(sv[i], scale_log2e, -m_new));
+    l_run *= by;
+    if constexpr (BYTES) {
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i & 1] += sv[i];
+      l_run += sum[0] + sum[1];
+      by_scale(sv, vs);
     }
-    l_run = __builtin_fmaf(l_run, by, sum[0] + sum[1]);
-    if constexpr (BYTES) by_scale(sv, vs);
 #pragma unroll
     for (int i = 0; i < 8; ++i) p.w[i] = pack_bf16(sv[2 * i], sv[2 * i + 1]);
+    if constexpr (!BYTES) {                                // the sum of the weights as the product has them: two at a time
+      const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+      float other = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, p.w[i]), ones, l_run, false);
+        other = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, p.w[i + 1]), ones, other, false);
+      }
+      l_run += other;
+    }
   };
   // step: logits of the next 32 tokens -> nxt, output of the ones before (pp), weights of these (cur -> pc)
-  auto step = [&](f32x16_t& cur, f32x16_t& nxt, const Weights& pp, Weights& pc, const unsigned char* k_next, const unsigned char* v_last, int n0, const float* ks,
-                  const float* vs, auto masked) FASA_INLINE {
+  auto step = [&](f32x16_t& cur, f32x16_t& nxt, const Weights& pp, Weights& pc, int k_next, int v_last, int n0, const float* ks, const float* vs) FASA_INLINE {
     float by;
     logits(k_next, nxt);
     output(v_last, pp);
-    softmax(cur, pc, by, n0, ks, vs, masked);
-#ifdef FASA_SGB
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    }
-#endif
+    softmax(cur, pc, by, n0, ks, vs);
     if (__ballot(by != 1.f) != 0ull) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) oc[d] *= by;
@@ -437,49 +457,51 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
     const auto of_v = [](int r) { return swz_v(r); };
     float rsk = 0.f, rsv = 0.f;
     // K of tiles 0 and 1, V of tile 0; zeros for V of the tile before the first, which has no weights, but what 0 is multiplied by has to be a number
-    int blk0 = look_up(s0), blk1 = look_up(s0 + kWideTok), blk2 = look_up(s0 + 2 * kWideTok);
-    store_rows(smk, load_rows(Kh, s0, blk0), of_k);
-    store_rows(smv, load_rows(Vh, s0, blk0), of_v);
-    store_rows(smk + kTileBytes, load_rows(Kh, s0 + kWideTok, blk1), of_k);
+    Rows ra = rows_of(s0, look_up(s0)), rb = rows_of(s0 + kWideTok, look_up(s0 + kWideTok)), rc = rows_of(s0 + 2 * kWideTok, look_up(s0 + 2 * kWideTok));
+    store_rows(smk, load_rows(Kh, ra), of_k);
+    store_rows(smv, load_rows(Vh, ra), of_v);
+    store_rows(smk + kTileBytes, load_rows(Kh, rb), of_k);
     if constexpr (BYTES) {
-      ssk[lane] = load_scale(cv.ks, s0, blk0) * scale_log2e;                            // (all waves, the same)
-      ssv[lane] = load_scale(cv.vs, s0, blk0);
-      ssk[kWideTok + lane] = load_scale(cv.ks, s0 + kWideTok, blk1) * scale_log2e;
-      rsk = load_scale(cv.ks, s0 + 2 * kWideTok, blk2);
+      ssk[lane] = load_scale(ks_h, s0, ra) * scale_log2e;                               // (all waves, the same)
+      ssv[lane] = load_scale(vs_h, s0, ra);
+      ssk[kWideTok + lane] = load_scale(ks_h, s0 + kWideTok, rb) * scale_log2e;
+      rsk = load_scale(ks_h, s0 + 2 * kWideTok, rc);
     }
     for (int x = t; x < kTileBytes / 16; x += NT) reinterpret_cast<uint4*>(smv + (kDeepSlots - 1) * kTileBytes)[x] = make_uint4(0, 0, 0, 0);
-    u32xl raw = load_rows(Kh, s0 + 2 * kWideTok, blk2);
-    int blk3 = look_up(s0 + 3 * kWideTok);
+    u32xl raw = load_rows(Kh, rc);
+    int blks = look_up(s0 + 3 * kWideTok);
     __syncthreads();
-    logits(smk, sa);
-    int c0 = 0, c1 = 1, c2 = 2;                            // slots of tiles T, T + 1, T + 2 (= T - 1)
-    const int n_plain = max(0, min(n_tiles, (wave_all - s0) / kWideTok));   // tiles without a mask
-    // before tile T: raw is K of tile T + 2; blk1 .. blk3: blocks of tiles T + 1 .. T + 3
-    auto tile = [&](int T, auto masked) FASA_INLINE {
+    logits(0, sa);
+    // Tile T, in slot c0 (c1, c2: slots of T + 1 and T + 2, the latter T - 1's too).  Before it: raw is K of tile T + 2, r1 and r2 are the rows of T + 1 and T + 2,
+    // blks the blocks of T + 3, whose rows r0 becomes.
+    auto tile = [&](int T, int c0, int c1, int c2, Rows& r0, const Rows& r1) FASA_INLINE {
+      constexpr int B = kTileBytes;
       const int j0 = s0 + T * kWideTok;
-      store_rows(smk + c2 * kTileBytes, raw, of_k);
-      raw = load_rows(Vh, j0 + kWideTok, blk1);
+      store_rows(smk + c2 * B, raw, of_k);
+      raw = load_rows(Vh, r1);
       if constexpr (BYTES) {
         ssk[c2 * kWideTok + lane] = rsk * scale_log2e;
-        rsv = load_scale(cv.vs, j0 + kWideTok, blk1);
+        rsv = load_scale(vs_h, j0 + kWideTok, r1);
       }
-      step(sa, sb, pa, pb, smk + c0 * kTileBytes + 32 * 256, smv + c2 * kTileBytes + 32 * 256, j0, ssk + c0 * kWideTok, ssv + c0 * kWideTok, masked);
-      store_rows(smv + c1 * kTileBytes, raw, of_v);
-      raw = load_rows(Kh, j0 + 3 * kWideTok, blk3);
+      step(sa, sb, pa, pb, c0 * B + 32 * 256, c2 * B + 32 * 256, j0, ssk + c0 * kWideTok, ssv + c0 * kWideTok);
+      store_rows(smv + c1 * B, raw, of_v);
+      r0 = rows_of(j0 + 3 * kWideTok, blks);
+      raw = load_rows(Kh, r0);
       if constexpr (BYTES) {
         ssv[c1 * kWideTok + lane] = rsv;
-        rsk = load_scale(cv.ks, j0 + 3 * kWideTok, blk3);
+        rsk = load_scale(ks_h, j0 + 3 * kWideTok, r0);
       }
-      blk1 = blk2; blk2 = blk3;
-      blk3 = look_up(j0 + 4 * kWideTok);
-      step(sb, sa, pb, pa, smk + c1 * kTileBytes, smv + c0 * kTileBytes, j0 + 32, ssk + c0 * kWideTok + 32, ssv + c0 * kWideTok + 32, masked);
+      blks = look_up(j0 + 4 * kWideTok);
+      step(sb, sa, pb, pa, c1 * B, c0 * B, j0 + 32, ssk + c0 * kWideTok + 32, ssv + c0 * kWideTok + 32);
       __syncthreads();
-      const int c = c0; c0 = c1; c1 = c2; c2 = c;
     };
-    // every wave runs all tiles, for the barriers
-    for (int T = 0; T < n_plain; ++T) tile(T, std::false_type{});
-    for (int T = n_plain; T < n_tiles; ++T) tile(T, std::true_type{});
-    output(smv + c2 * kTileBytes + 32 * 256, pa);
+    int c0 = 0, c1 = 1, c2 = 2;
+    for (int T = 0; T < n_tiles; ++T) {
+      tile(T, c0, c1, c2, ra, rb);
+      const Rows r = ra; ra = rb; rb = rc; rc = r;
+      const int c = c0; c0 = c1; c1 = c2; c2 = c;
+    }
+    output(c2 * kTileBytes + 32 * 256, pa);
   }
   l_run = xor32_sum(l_run);
   if (32 * wave + col >= rows) return;
@@ -561,7 +583,8 @@ hipError_t launch_chunk_wide(const fasa_shape& s, const ChunkPlan& p, const Chun
   if (p.tile_rows == 128)
     return a.fmt == kPlain ? wide_t<kPlain, 4>(s, p, a, st) : a.fmt == kInt8 ? wide_t<kInt8, 4>(s, p, a, st) : wide_t<kE4m3, 4>(s, p, a, st);
   // pages of fewer tokens than a wave's load has rows, or rows far apart: tokens are looked up one by one
-  const bool apart = (a.cv.pm.table != nullptr && (1 << a.cv.pm.shift) < (a.fmt == kPlain ? 4 : 8)) || a.cv.sn >= (1ll << 28);
+  const bool apart = (a.cv.pm.table != nullptr && (1 << a.cv.pm.shift) < (a.fmt == kPlain ? 4 : 8)) ||
+                     a.cv.sn >= (1ll << 27) || a.cv.sb >= (1ll << 31);
   if (apart) return a.fmt == kPlain ? wide_t<kPlain, 8>(s, p, a, st) : a.fmt == kInt8 ? wide_t<kInt8, 8>(s, p, a, st) : wide_t<kE4m3, 8>(s, p, a, st);
   return a.fmt == kPlain ? deep_t<kPlain>(s, p, a, st) : a.fmt == kInt8 ? deep_t<kInt8>(s, p, a, st) : deep_t<kE4m3>(s, p, a, st);
 }
