@@ -514,9 +514,9 @@ struct ChunkLayout {
   size_t acc_off, ml_off, total;
 };
 // The part of the workspace that has to be zero comes first, where the other calls have it; the partial results behind it.
-ChunkLayout chunk_layout(fasa_shape s, const ChunkView& ch) {
+ChunkLayout chunk_layout(fasa_shape s, const ChunkView& ch, bool apart) {
   ChunkLayout L;
-  L.plan = plan_chunk(s, ch.n_new, ch.n_rows, ch.row_start != nullptr);
+  L.plan = plan_chunk(s, apart, ch.n_new, ch.n_rows, ch.row_start != nullptr);
   s.budget = s.n_ctx;                     // (any: that part does not depend on it)
   const WsLayout w = ws_layout(s);
   L.acc_off = w.cand_off;
@@ -559,8 +559,8 @@ int fasa_cache_read(const fasa_shape* shape, const fasa_paging* paging, const fa
 size_t fasa_chunk_workspace_bytes(const fasa_shape* shape, const fasa_chunk* chunk) {
   ChunkView ch;
   if (check_shape(shape, kNeedCtx | kNeedBudget) != FASA_OK || check_chunk(chunk, shape, 0, &ch) != FASA_OK) return 0;
-  // (fasa_workspace_init asks for as much as the other calls need)
-  return std::max(chunk_layout(*shape, ch).total, ws_layout(*shape).total);
+  // (of any cache; fasa_workspace_init asks for as much as the other calls need)
+  return std::max({chunk_layout(*shape, ch, false).total, chunk_layout(*shape, ch, true).total, ws_layout(*shape).total});
 }
 
 int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const fasa_chunk* chunk,
@@ -574,7 +574,7 @@ int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const 
   rc = check_chunk(chunk, shape, kOfQuery, &ch);
   if (rc != FASA_OK) return rc;
   if (!q || !O || !ws || !aligned16(q) || !aligned16(O) || !aligned16(ws)) return FASA_EINVAL;
-  const ChunkLayout L = chunk_layout(*shape, ch);
+  const ChunkLayout L = chunk_layout(*shape, ch, chunk_rows_apart(cv, (CacheFmt)cache->format));
   if (ws_bytes < L.total) return FASA_EWORKSPACE;
   char* base = (char*)ws;
   const ChunkArgs a{cv, ch, (CacheFmt)cache->format, q, O, chunk->q_stride, chunk->o_stride, (float*)(base + L.acc_off),

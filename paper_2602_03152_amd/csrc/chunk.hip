@@ -261,25 +261,10 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
 }
 
 // Splits: as many as fill the compute units once, of 64 tokens or more, 256 at most (the merge's weights lie in LDS).
-ChunkPlan plan_chunk(const fasa_shape& s, int n_new, int n_rows, bool by_row_start) {
+ChunkPlan plan_chunk(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start) {
   ChunkPlan p{};
   const int G = s.n_q_heads / s.n_kv_heads;
-  const long long m = (long long)n_new * G;
-  p.wide = s.dtype == FASA_BF16 && m > kChunkRows;
-  if (p.wide) {
-    p.tile_rows = m <= 128 ? 128 : 256;
-    p.tiles = (int)chunk_tiles(by_row_start, s.batch, n_new, n_rows, G, p.tile_rows);
-    p.per_seq = (int)((m + p.tile_rows - 1) / p.tile_rows);
-    long long n = kAssumedCUs * (p.tile_rows == 128 ? 2 : 1) / ((long long)p.tiles * s.n_kv_heads);
-    const int most = (s.n_ctx + 255) / 256;
-    if (n > most) n = most;
-    if (n > 64) n = 64;
-    p.splits = n < 1 ? 1 : (int)n;
-    const size_t parts = p.splits == 1 ? 0 : (size_t)s.batch * s.n_kv_heads * p.per_seq * p.splits * p.tile_rows;
-    p.part_acc_bytes = parts * kHeadDim * 4;
-    p.part_ml_bytes = parts * 8;
-    return p;
-  }
+  if (s.dtype == FASA_BF16 && (long long)n_new * G > kChunkRows) return plan_chunk_wide(s, apart, n_new, n_rows, by_row_start);
   p.tile_rows = n_new * (long long)G < kChunkRows ? n_new * G : kChunkRows;
   p.tiles = (int)chunk_tiles(by_row_start, s.batch, n_new, n_rows, G, kChunkRows);
   p.per_seq = (int)(((long long)n_new * G + kChunkRows - 1) / kChunkRows);

@@ -119,11 +119,17 @@ hipError_t launch_cache_read(const fasa_shape& s, const CacheView& cv, CacheFmt 
 // How a chunk is attended.  wide: by chunk_wide.hip.  tiles: of the grid; per_seq: query tiles of the longest sequence; splits: of a tile's tokens.
 struct ChunkPlan {
   bool wide;
+  bool apart;         // wide: rows are looked up one by one
   int tile_rows;      // query rows (new token, head of the group) of a tile
   int tiles, per_seq, splits;
   size_t part_acc_bytes, part_ml_bytes;
 };
-ChunkPlan plan_chunk(const fasa_shape& s, int n_new, int n_rows, bool by_row_start);
+// apart: chunk_wide.hip has to look rows up one by one - pages of fewer tokens than a wave's load has rows, or strides beyond what it multiplies in 32 bits
+inline bool chunk_rows_apart(const CacheView& cv, CacheFmt fmt) {
+  return (cv.pm.table != nullptr && ((1 << cv.pm.shift) < (fmt == kPlain ? 4 : 8) || cv.sb >= (1ll << 31))) || cv.sn >= (1ll << 27);
+}
+ChunkPlan plan_chunk(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start);
+ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start);
 struct ChunkArgs {
   CacheView cv;
   ChunkView ch;

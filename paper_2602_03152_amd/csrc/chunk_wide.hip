@@ -1,5 +1,5 @@
 // Attention of a chunk of bf16 query rows over a bf16 or 8-bit cache: many query rows of a KV head (new token, head of the group) against the same K and V,
-// both products on the matrix cores, K and V tiles of 64 tokens shared by the workgroup through LDS.
+// both products on the matrix cores, tiles of 64 tokens of K and V shared by the workgroup through LDS, a wave for every 32 query rows.
 //
 //   S^T = K Q^T   (tokens x queries; 32 x 32 x 16 MFMAs, K from LDS, Q in registers): the result's column, a lane's own, is one query, its 16
 //                 registers are tokens 8 (i / 4) + 4 (lane / 32) + i % 4.  Maximum, exponentials and sum of a query are the lane's own but for one exchange
@@ -8,13 +8,14 @@
 //                 8 s .. 8 s + 7 of k-step s.  V^T with tokens in that order comes out of LDS by transposing reads (ds_read_b64_tr_b16: 16 lanes get
 //                 one column each of four rows).  A new maximum rescales a lane's own accumulators.
 // LDS rows are 256 bytes of 16-byte chunks; chunk c of token t is stored at c ^ (t mod 16) (K) or c ^ 2 (t mod 8) (V), so that the lanes
-// of a read fall on all banks.
+// of a read fall on all banks.  8-bit rows become bf16 (exactly) on their way into LDS, once for all waves; their scales multiply logits and weights in float32.
 #include "chunk_common.h"
 
 namespace fasa {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) const unsigned char* lds_ptr;
 
 constexpr int kWideTok = 64;                              // tokens of a tile
 constexpr int kTileBytes = kWideTok * kHeadDim * 2;       // of K or V in LDS
@@ -23,339 +24,123 @@ __device__ __forceinline__ int swz_k(int t) { return t & 15; }
 __device__ __forceinline__ int swz_v(int t) { return 2 * (t & 7); }
 
 // Four bf16 of one column of V for each of 16 lanes, out of four rows of LDS
-__device__ __forceinline__ uint2 lds_read_tr(__attribute__((address_space(3))) const unsigned char* p) {
+__device__ __forceinline__ uint2 lds_read_tr(lds_ptr p) {
   const s16x4_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)p);
   return __builtin_bit_cast(uint2, r);
 }
 
-template <CacheFmt F, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void chunk_wide_kernel(const uint16_t* __restrict__ q, const typename RowType<uint16_t, F>::type* __restrict__ K,
-                                                                const typename RowType<uint16_t, F>::type* __restrict__ V, uint16_t* __restrict__ O,
-                                                                float* __restrict__ part_acc, float2* __restrict__ part_ml, CacheView cv, ChunkView ch,
-                                                                int batch, int Hkv, int G, int tiles_each, int splits, long long q_stride,
-                                                                long long o_stride, float scale_log2e) {
-  constexpr int D = kHeadDim, NT = 64 * NW, TR = 32 * NW;
-  constexpr bool BYTES = F != kPlain;
+// What a workgroup works on: query rows [qt TR, qt TR + rows) of sequence b and KV head h, tokens [s0, s1).
+template <int TR> struct WideJob {
+  int b, h, qt, split, rows, row0, pos0, s0, s1, n_tiles;
+  __device__ __forceinline__ int token_of(int r, int G) const { return (qt * TR + r) / G; }      // new token of the tile's row r
+  // False: nothing to do.  Workgroups: heads fastest (those of a sequence read the same blocks, and a head's lie on one XCD where there are eight), then splits.
+  __device__ __forceinline__ bool find(const ChunkView& ch, int batch, int Hkv, int G, int tiles_each, int splits) {
+    unsigned id = blockIdx.x;
+    h = (int)(id % (unsigned)Hkv);
+    id /= (unsigned)Hkv;
+    split = (int)(id % (unsigned)splits);
+    id /= (unsigned)splits;
+    if (!find_chunk_tile<TR>(ch, batch, G, tiles_each, id, b, qt)) return false;
+    const SeqChunk sc = seq_chunk(ch, b);
+    const int m = sc.n_new * G, m_tiles = (m + TR - 1) / TR;
+    if (qt >= m_tiles) return false;
+    qt = m_tiles - 1 - qt;                                 // the longest first
+    rows = min(TR, m - qt * TR);
+    row0 = sc.row;
+    pos0 = sc.n_ctx - sc.n_new;
+    const int seen = pos0 + token_of(rows - 1, G) + 1;     // tokens that the tile's last row sees
+    const int share = ((seen + splits - 1) / splits + kWideTok - 1) / kWideTok * kWideTok;
+    s0 = min(split * share, seen);
+    s1 = min(seen, s0 + share);
+    n_tiles = (s1 - s0 + kWideTok - 1) / kWideTok;
+    return true;
+  }
+};
+
+// Rows of the cache, 16 bytes a lane and load, into registers and on to LDS.
+// A wave's load is WROWS rows, which lie in one block (pages of that many tokens or more): where they begin is the wave's, in scalar registers, and the same for K
+// and V; what is a lane's is its row and piece in there, clamped to the last row that there is.  Lane l looks up the block of a tile's token l, a tile or more
+// ahead of the rows: a lookup between two loads would wait for the first one's.  APART: smaller pages (or strides that 32 bits do not hold): every lane
+// finds its own rows.
+template <CacheFmt F, int NW, bool APART> struct WideLoader {
+  static constexpr bool BYTES = F != kPlain;
   using RT = typename RowType<uint16_t, F>::type;
-  constexpr int PER_ROW = BYTES ? 8 : 16;                 // 16-byte pieces of a stored row
-  constexpr int NL = kWideTok * PER_ROW / NT;             // pieces of K, and of V, a thread
-  extern __shared__ __align__(16) unsigned char smem[];   // [2][K tile, V tile], then scales [2][k 64, v 64]
-  float* sm_scale = reinterpret_cast<float*>(smem + 4 * kTileBytes);
-
-  unsigned id = blockIdx.x;
-  const int h = (int)(id % (unsigned)Hkv);
-  id /= (unsigned)Hkv;
-  const int split = (int)(id % (unsigned)splits);
-  id /= (unsigned)splits;
-  int b, qt;
-  if (!find_chunk_tile<TR>(ch, batch, G, tiles_each, id, b, qt)) return;
-  const SeqChunk sc = seq_chunk(ch, b);
-  const int m = sc.n_new * G, m_tiles = (m + TR - 1) / TR;
-  if (qt >= m_tiles) return;
-  qt = m_tiles - 1 - qt;                                   // the longest first
-  const int rows = min(TR, m - qt * TR);
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int col = lane & 31, half = lane >> 5;
-  const int pos0 = sc.n_ctx - sc.n_new;
-  const auto token_of = [&](int r) FASA_INLINE { return (qt * TR + r) / G; };
-  const int seen = pos0 + token_of(rows - 1) + 1;          // tokens that the tile's last row sees
-  const int share = ((seen + splits - 1) / splits + kWideTok - 1) / kWideTok * kWideTok;
-  const int s0 = min(split * share, seen), s1 = min(seen, s0 + share);
-  const int n_tiles = (s1 - s0 + kWideTok - 1) / kWideTok;
-
-  // this lane's query
-  const int my = min(32 * wave + col, rows - 1), my_tok = token_of(my);
-  const int my_end = min(s1, pos0 + my_tok + 1);
-  const int wave_all = min(s1, pos0 + token_of(min(32 * wave, rows - 1)) + 1);         // tokens that all of the wave's queries see
-  const int wave_end = 32 * wave < rows ? min(s1, pos0 + token_of(min(32 * wave + 31, rows - 1)) + 1) : s0;
-  bf16x8_t qb[8];
-  {
-    const uint16_t* p = q + (long long)(sc.row + my_tok) * q_stride + (long long)(h * G + (qt * TR + my) - my_tok * G) * D + 8 * half;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) qb[i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(p + 16 * i));
-  }
-  f32x16_t oc[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) oc[i] = f32x16_t{};
-  float m_run = kNegBig, l_run = 0.f;
-
-  // ---- loader: piece x of a tile is 16 bytes of row x / PER_ROW ----
-  uint4 rk[NL], rv[NL];
-  float rs = 0.f;                                          // threads 0-63: scale of K row t, 64-127: of V row t - 64
-  const RT* Kh = K + h * cv.sh;
-  const RT* Vh = V + h * cv.sh;
-  // A tile's blocks are looked up a tile ahead of its loads: a lookup between loads would wait for all loads before it.
-  int blk[NL], sblk = 0;
-  auto look_up = [&](int j0) FASA_INLINE {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) blk[i] = cache_block(cv.pm, b, min(j0 + (t + NT * i) / PER_ROW, s1 - 1));
-    if constexpr (BYTES) sblk = cache_block(cv.pm, b, min(j0 + (t & 63), s1 - 1));
-  };
-  auto load_tile = [&](int j0) FASA_INLINE {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int x = t + NT * i;
-      const long long at = cache_clamp(cv.pm, blk[i]) * cv.sb + cache_offset(cv.pm, min(j0 + x / PER_ROW, s1 - 1)) * cv.sn + (x % PER_ROW) * (16 / (int)sizeof(RT));
-      rk[i] = *reinterpret_cast<const uint4*>(Kh + at);
-      rv[i] = *reinterpret_cast<const uint4*>(Vh + at);
-    }
-    if constexpr (BYTES) {
-      if (t < 2 * kWideTok) rs = (t < kWideTok ? cv.ks : cv.vs)[cache_clamp(cv.pm, sblk) * cv.ssb + h * cv.ssh + cache_offset(cv.pm, min(j0 + (t & 63), s1 - 1))];
-    }
-    look_up(j0 + kWideTok);
-  };
-  auto store_tile = [&](int buf) FASA_INLINE {
-    unsigned char* k = smem + buf * 2 * kTileBytes;
-    unsigned char* v = k + kTileBytes;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int x = t + NT * i, r = x / PER_ROW, c = x % PER_ROW;
-      if constexpr (BYTES) {
-        const uint32_t wk[4] = {rk[i].x, rk[i].y, rk[i].z, rk[i].w}, wv[4] = {rv[i].x, rv[i].y, rv[i].z, rv[i].w};
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint2 ka = bytes_to_bf16<F>(wk[2 * j]), kb = bytes_to_bf16<F>(wk[2 * j + 1]);
-          const uint2 va = bytes_to_bf16<F>(wv[2 * j]), vb = bytes_to_bf16<F>(wv[2 * j + 1]);
-          *reinterpret_cast<uint4*>(k + r * 256 + (((2 * c + j) ^ swz_k(r)) << 4)) = make_uint4(ka.x, ka.y, kb.x, kb.y);
-          *reinterpret_cast<uint4*>(v + r * 256 + (((2 * c + j) ^ swz_v(r)) << 4)) = make_uint4(va.x, va.y, vb.x, vb.y);
-        }
-      } else {
-        *reinterpret_cast<uint4*>(k + r * 256 + ((c ^ swz_k(r)) << 4)) = rk[i];
-        *reinterpret_cast<uint4*>(v + r * 256 + ((c ^ swz_v(r)) << 4)) = rv[i];
-      }
-    }
-    if constexpr (BYTES) {
-      if (t < 2 * kWideTok) sm_scale[buf * 2 * kWideTok + t] = t < kWideTok ? rs * scale_log2e : rs;
-    }
-  };
-
-  if (n_tiles > 0) {
-    look_up(s0);
-    load_tile(s0);
-    store_tile(0);
-    if (n_tiles > 1) load_tile(s0 + kWideTok);
-    __syncthreads();
-  }
-  for (int j = 0; j < n_tiles; ++j) {
-    const int j0 = s0 + j * kWideTok, buf = j & 1;
-    const unsigned char* kt = smem + buf * 2 * kTileBytes;
-    const unsigned char* vt = kt + kTileBytes;
-    const bool work = j0 < wave_end;
-    f32x16_t sv[2];
-    if (work) {
-      sv[0] = f32x16_t{};
-      sv[1] = f32x16_t{};
-#pragma unroll
-      for (int s = 0; s < 8; ++s)
-#pragma unroll
-        for (int nb = 0; nb < 2; ++nb) {
-          const int r = 32 * nb + col;
-          const uint4 a = *reinterpret_cast<const uint4*>(kt + r * 256 + (((2 * s + half) ^ swz_k(r)) << 4));
-          sv[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), qb[s], sv[nb], 0, 0, 0);
-        }
-    }
-    if (j + 1 < n_tiles) store_tile(buf ^ 1);
-    if (j + 2 < n_tiles) load_tile(j0 + 2 * kWideTok);
-    if (work) {
-      float mul = scale_log2e;
-      if constexpr (BYTES) {
-        const float* ks = sm_scale + buf * 2 * kWideTok;
-#pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float4 f = *reinterpret_cast<const float4*>(ks + 32 * nb + 8 * g + 4 * half);
-            sv[nb][4 * g] *= f.x; sv[nb][4 * g + 1] *= f.y; sv[nb][4 * g + 2] *= f.z; sv[nb][4 * g + 3] *= f.w;
-          }
-        mul = 1.f;
-      }
-      if (j0 + kWideTok > wave_all) {
-#pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sv[nb][i] = j0 + 32 * nb + 8 * (i / 4) + 4 * half + i % 4 < my_end ? sv[nb][i] : -INFINITY;
-      }
-      float mx = sv[0][0];
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sv[nb][i]);
-      mx = xor32_max(mx) * mul;
-      const float m_new = fmaxf(m_run, mx);
-      if (__ballot(m_new != m_run) != 0ull) {
-        const float by = __builtin_amdgcn_exp2f(m_run - m_new);
-        m_run = m_new;
-        l_run *= by;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) oc[d] *= by;
-      }
-      uint32_t pw[2][8];
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sv[nb][i] = __builtin_amdgcn_exp2f(BYTES ? sv[nb][i] - m_new : __builtin_fmaf(sv[nb][i], mul, -m_new));
-          l_run += sv[nb][i];
-        }
-        if constexpr (BYTES) {
-          const float* vs = sm_scale + buf * 2 * kWideTok + kWideTok;
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float4 f = *reinterpret_cast<const float4*>(vs + 32 * nb + 8 * g + 4 * half);
-            sv[nb][4 * g] *= f.x; sv[nb][4 * g + 1] *= f.y; sv[nb][4 * g + 2] *= f.z; sv[nb][4 * g + 3] *= f.w;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pw[nb][i] = pack_bf16(sv[nb][2 * i], sv[nb][2 * i + 1]);
-      }
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bf16x8_t p = __builtin_bit_cast(bf16x8_t, make_uint4(pw[s / 2][4 * (s & 1)], pw[s / 2][4 * (s & 1) + 1], pw[s / 2][4 * (s & 1) + 2], pw[s / 2][4 * (s & 1) + 3]));
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const int r = 16 * s + 4 * half + ((lane & 15) >> 2), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-          const unsigned char* at = vt + ((c ^ swz_v(r)) << 4) + 8 * (lane & 1) + r * 256;
-          const unsigned char* at8 = vt + ((c ^ swz_v(r + 8)) << 4) + 8 * (lane & 1) + (r + 8) * 256;
-          const uint2 lo = lds_read_tr((__attribute__((address_space(3))) const unsigned char*)at), hi = lds_read_tr((__attribute__((address_space(3))) const unsigned char*)at8);
-          oc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)), p, oc[d], 0, 0, 0);
-        }
-      }
-    }
-    __syncthreads();
-  }
-  l_run = xor32_sum(l_run);
-  if (32 * wave + col >= rows) return;
-  if (splits == 1) {
-    const float by = 1.0f / l_run;
-    uint16_t* o = O + (long long)(sc.row + my_tok) * o_stride + (long long)(h * G + (qt * TR + my) - my_tok * G) * D + 4 * half;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<uint2*>(o + 32 * d + 8 * g) = make_uint2(pack_bf16(oc[d][4 * g] * by, oc[d][4 * g + 1] * by), pack_bf16(oc[d][4 * g + 2] * by, oc[d][4 * g + 3] * by));
-    return;
-  }
-  const size_t at = (((size_t)(b * Hkv + h) * tiles_each + qt) * splits + split) * TR + my;
-  float* pa = part_acc + at * D + 4 * half;
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<float4*>(pa + 32 * d + 8 * g) = make_float4(oc[d][4 * g], oc[d][4 * g + 1], oc[d][4 * g + 2], oc[d][4 * g + 3]);
-  if (half == 0) part_ml[at] = make_float2(m_run, l_run);
-}
-
-// largest of a lane's sixteen logits
-__device__ __forceinline__ float largest(const f32x16_t& v) {
-  float m = __builtin_fmaxf(v[0], v[1]);
-#pragma unroll
-  for (int i = 2; i < 16; i += 2) m = __builtin_fmaxf(m, __builtin_fmaxf(v[i], v[i + 1]));
-  return m;
-}
-
-// The same for long chunks, eight waves of 32 queries (256 rows a tile), two a SIMD.  In steps of 32 tokens: step u runs the logits of step u + 1 and the
-// output of step u - 1 beside its own exponentials, in one block of straight code, so that the matrix cores have work while a wave is at its softmax.
-constexpr int kDeepWaves = 8, kDeepRows = 32 * kDeepWaves;
-constexpr int kDeepSlots = 3;                             // tiles of K, and of V, in LDS: K of tiles T, T + 1 and V of T - 1, T are read while K of T + 2 and V of T + 1 are written
-template <CacheFmt F>
-__global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const uint16_t* __restrict__ q, const typename RowType<uint16_t, F>::type* __restrict__ K,
-                                                            const typename RowType<uint16_t, F>::type* __restrict__ V, uint16_t* __restrict__ O,
-                                                            float* __restrict__ part_acc, float2* __restrict__ part_ml, CacheView cv, ChunkView ch,
-                                                            int batch, int Hkv, int G, int tiles_each, int splits, long long q_stride,
-                                                            long long o_stride, float scale_log2e) {
-  constexpr int D = kHeadDim, NT = 64 * kDeepWaves, TR = kDeepRows;
-  constexpr bool BYTES = F != kPlain;
-  using RT = typename RowType<uint16_t, F>::type;
-  constexpr int PER_ROW = BYTES ? 8 : 16;                 // 16-byte pieces of a stored row
-  constexpr int NL = kWideTok * PER_ROW / NT;             // pieces of K, and of V, a thread
-  constexpr int WROWS = 64 / PER_ROW;                     // rows of a wave's load
-  extern __shared__ __align__(16) unsigned char smem[];   // [slot] K tiles, [slot] V tiles, then scales [slot][k 64], [slot][v 64]
-  unsigned char* const smk = smem;
-  unsigned char* const smv = smem + kDeepSlots * kTileBytes;
-  float* const ssk = reinterpret_cast<float*>(smem + 2 * kDeepSlots * kTileBytes);
-  float* const ssv = ssk + kDeepSlots * kWideTok;
-
-  unsigned id = blockIdx.x;
-  const int h = (int)(id % (unsigned)Hkv);
-  id /= (unsigned)Hkv;
-  const int split = (int)(id % (unsigned)splits);
-  id /= (unsigned)splits;
-  int b, qt;
-  if (!find_chunk_tile<TR>(ch, batch, G, tiles_each, id, b, qt)) return;
-  const SeqChunk sc = seq_chunk(ch, b);
-  const int m = sc.n_new * G, m_tiles = (m + TR - 1) / TR;
-  if (qt >= m_tiles) return;
-  qt = m_tiles - 1 - qt;                                   // the longest first
-  const int rows = min(TR, m - qt * TR);
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int col = lane & 31, half = lane >> 5;
-  const int pos0 = sc.n_ctx - sc.n_new;
-  const auto token_of = [&](int r) FASA_INLINE { return (qt * TR + r) / G; };
-  const int seen = pos0 + token_of(rows - 1) + 1;          // tokens that the tile's last row sees
-  const int share = ((seen + splits - 1) / splits + kWideTok - 1) / kWideTok * kWideTok;
-  const int s0 = min(split * share, seen), s1 = min(seen, s0 + share);
-  const int n_tiles = (s1 - s0 + kWideTok - 1) / kWideTok;
-
-  // this lane's query
-  const int my = min(32 * wave + col, rows - 1), my_tok = token_of(my);
-  const int my_end = min(s1, pos0 + my_tok + 1);
-  const int wave_all = min(s1, pos0 + token_of(min(32 * wave, rows - 1)) + 1);         // tokens that all of the wave's queries see
-  bf16x8_t qb[8];
-  {
-    const uint16_t* p = q + (long long)(sc.row + my_tok) * q_stride + (long long)(h * G + (qt * TR + my) - my_tok * G) * D + 8 * half;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) qb[i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(p + 16 * i));
-  }
-  f32x16_t oc[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) oc[i] = f32x16_t{};
-  float m_run = kNegBig, l_run = 0.f;
-
-  // ---- loader ----
-  // A wave's load is WROWS rows, which lie in one block (pages of that many tokens or more): where they begin is the wave's, in scalar registers, and the same for
-  // K and V; what is a lane's is its row and piece in there, clamped to the last row that there is.  Lane l looks up the block of a tile's token l.
-  const bool paged = cv.pm.table != nullptr;
-  const int32_t* const table = paged ? cv.pm.table + (size_t)b * cv.pm.max_blocks : reinterpret_cast<const int32_t*>(q);
-  const int shift = paged ? cv.pm.shift : 31, in_block = paged ? (1 << cv.pm.shift) - 1 : 0x7fffffff;
-  const int blk_max = paged ? cv.pm.n_pool - 1 : 0;
-  const uint32_t blk_bytes = paged ? (uint32_t)(cv.sb * (int)sizeof(RT)) : 0, row_bytes = (uint32_t)(cv.sn * (int)sizeof(RT));
-  const long long seq = (paged ? 0 : b * cv.sb) + h * cv.sh;
-  const char* const Kh = reinterpret_cast<const char*>(K + seq);
-  const char* const Vh = reinterpret_cast<const char*>(V + seq);
-  const uint32_t my_row = (uint32_t)(lane / PER_ROW) * row_bytes, my_piece = (uint32_t)(lane % PER_ROW) * 16;
+  static constexpr int PER_ROW = BYTES ? 8 : 16;           // 16-byte pieces of a stored row
+  static constexpr int NL = kWideTok * PER_ROW / (64 * NW);     // pieces of K, and of V, a thread
+  static constexpr int WROWS = 64 / PER_ROW;               // rows of a wave's load
   typedef uint32_t u32xl __attribute__((ext_vector_type(4 * NL)));
-  struct Rows { uint64_t at[NL]; uint32_t last[NL]; int blk; };     // of a tile: where this wave's loads begin, bytes to the last row of them; lane l: block of token l
-  auto look_up = [&](int j0) FASA_INLINE { return table[min(j0 + lane, s1 - 1) >> shift]; };
-  auto rows_of = [&](int j0, int blks) FASA_INLINE {
+  struct Rows {                                            // of a tile: where this wave's loads begin (APART: this lane's), bytes from there to the last row
+    uint64_t at[NL];
+    uint32_t last[NL];
+    int blk;                                               // lane l: block of token l
+  };
+  const int32_t* table;
+  const char *Kh, *Vh;
+  const float *ks, *vs;
+  long long ssb, sb, sn;
+  uint32_t blk_bytes, row_bytes, my_row, my_piece;
+  int shift, in_block, blk_max, s1, wave, lane;
+
+  __device__ __forceinline__ WideLoader(const CacheView& cv, const void* K, const void* V, const void* any, int b, int h, int s1_, int wave_, int lane_) {
+    const bool paged = cv.pm.table != nullptr;
+    table = paged ? cv.pm.table + (size_t)b * cv.pm.max_blocks : reinterpret_cast<const int32_t*>(any);     // (an entry is read in any case)
+    shift = paged ? cv.pm.shift : 31;
+    in_block = paged ? (1 << cv.pm.shift) - 1 : 0x7fffffff;
+    blk_max = paged ? cv.pm.n_pool - 1 : 0;
+    const long long seq = (paged ? 0 : b * cv.sb) + h * cv.sh;
+    Kh = reinterpret_cast<const char*>((const RT*)K + seq);
+    Vh = reinterpret_cast<const char*>((const RT*)V + seq);
+    sb = paged ? cv.sb * (int)sizeof(RT) : 0;
+    sn = cv.sn * (int)sizeof(RT);
+    blk_bytes = (uint32_t)sb;
+    row_bytes = (uint32_t)sn;
+    if constexpr (BYTES) {
+      ks = cv.ks + (paged ? 0 : b * cv.ssb) + h * cv.ssh;
+      vs = cv.vs + (paged ? 0 : b * cv.ssb) + h * cv.ssh;
+      ssb = paged ? cv.ssb : 0;
+    }
+    s1 = s1_;
+    wave = wave_;
+    lane = lane_;
+    my_row = (uint32_t)(lane / PER_ROW) * row_bytes;
+    my_piece = (uint32_t)(lane % PER_ROW) * 16;
+  }
+  // the table's entry for token j0 + lane (tokens behind the last one: the last one's)
+  __device__ __forceinline__ int look_up(int j0) const { return table[min(j0 + lane, s1 - 1) >> shift]; }
+  __device__ __forceinline__ Rows rows_of(int j0, int entry) const {
     Rows r;
-    r.blk = min(max(blks, 0), blk_max);
+    r.blk = min(max(entry, 0), blk_max);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int g = min(j0 + WROWS * (wave + kDeepWaves * i), (s1 - 1) & ~(WROWS - 1));
-      const uint32_t blk = (uint32_t)__builtin_amdgcn_readlane(r.blk, max(g - j0, 0));
-      r.at[i] = (uint64_t)blk * blk_bytes + (uint64_t)(uint32_t)(g & in_block) * row_bytes;
-      r.last[i] = (uint32_t)min(s1 - 1 - g, WROWS - 1) * row_bytes;
+      if constexpr (APART) {
+        const int n = min(j0 + WROWS * (wave + NW * i) + lane / PER_ROW, s1 - 1);
+        const int blk = __shfl(r.blk, max(n - j0, 0));
+        r.at[i] = (uint64_t)(blk * sb + (n & in_block) * sn);
+        r.last[i] = 0;
+      } else {
+        const int g = min(j0 + WROWS * (wave + NW * i), (s1 - 1) & ~(WROWS - 1));
+        const uint32_t blk = (uint32_t)__builtin_amdgcn_readlane(r.blk, max(g - j0, 0));
+        r.at[i] = (uint64_t)blk * blk_bytes + (uint64_t)(uint32_t)(g & in_block) * row_bytes;
+        r.last[i] = (uint32_t)min(s1 - 1 - g, WROWS - 1) * row_bytes;
+      }
     }
     return r;
-  };
-  auto load_rows = [&](const char* H, const Rows& r) FASA_INLINE {
+  }
+  __device__ __forceinline__ u32xl load(const char* H, const Rows& r) const {
     u32xl v;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const uint4 x = *reinterpret_cast<const uint4*>(H + r.at[i] + (min(my_row, r.last[i]) + my_piece));
+      const uint4 x = *reinterpret_cast<const uint4*>(H + r.at[i] + ((APART ? 0 : min(my_row, r.last[i])) + my_piece));
       v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
     }
     return v;
-  };
-  const float* const ks_h = BYTES ? cv.ks + (paged ? 0 : b * cv.ssb) + h * cv.ssh : nullptr;
-  const float* const vs_h = BYTES ? cv.vs + (paged ? 0 : b * cv.ssb) + h * cv.ssh : nullptr;
-  auto load_scale = [&](const float* s, int j0, const Rows& r) FASA_INLINE {
-    return s[r.blk * (paged ? cv.ssb : 0) + (min(j0 + lane, s1 - 1) & in_block)];
-  };
-  auto store_rows = [&](unsigned char* to, u32xl r, auto swz) FASA_INLINE {
+  }
+  // of token j0 + lane
+  __device__ __forceinline__ float load_scale(const float* s, int j0, const Rows& r) const { return s[r.blk * ssb + (min(j0 + lane, s1 - 1) & in_block)]; }
+  template <class Swz> __device__ __forceinline__ void store(unsigned char* to, u32xl r, Swz swz) const {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int row = WROWS * (wave + kDeepWaves * i) + lane / PER_ROW, c = lane % PER_ROW;
+      const int row = WROWS * (wave + NW * i) + lane / PER_ROW, c = lane % PER_ROW;
       if constexpr (BYTES) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -366,54 +151,85 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
         *reinterpret_cast<uint4*>(to + row * 256 + ((c ^ swz(row)) << 4)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
       }
     }
-  };
-
-  // ---- products ----
-  typedef __attribute__((address_space(3))) const unsigned char* lds_ptr;
-  lds_ptr k_at[8], v_at[4];                                // places of this lane's operands in slot 0, of its first 32 (16) tokens
-#pragma unroll
-  for (int s = 0; s < 8; ++s) k_at[s] = (lds_ptr)smk + col * 256 + (((2 * s + half) ^ swz_k(col)) << 4);
-#pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    const int r = 4 * half + ((lane & 15) >> 2), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    v_at[d] = (lds_ptr)smv + r * 256 + ((c ^ swz_v(r)) << 4) + 8 * (lane & 1);
   }
-  struct Weights { uint32_t w[8]; };
-  // at: where the 32 tokens begin, in bytes from slot 0
-  auto logits = [&](int at, f32x16_t& sv) FASA_INLINE {
+  __device__ __forceinline__ void store_k(unsigned char* to, u32xl r) const { store(to, r, [](int t) { return swz_k(t); }); }
+  __device__ __forceinline__ void store_v(unsigned char* to, u32xl r) const { store(to, r, [](int t) { return swz_v(t); }); }
+};
+
+// The 32 queries of a wave: products with tiles in LDS, softmax, result.
+template <bool BYTES> struct WideQueries {
+  struct Weights { uint32_t w[8]; };                       // of 32 tokens
+  bf16x8_t qb[8];
+  f32x16_t oc[4];
+  float m_run, l_run;                                      // of this lane's query (log2 domain); l_run over this lane's tokens
+  uint32_t k_at[8], v_at[4];                               // places of this lane's operands in a tile, of its first 32 (16) tokens
+  int my, my_end, all, half;                               // row in the tile, tokens that it sees, tokens that all rows of the wave see
+  long long at;                                            // of the row, in elements of q
+
+  template <int TR>
+  __device__ __forceinline__ WideQueries(const WideJob<TR>& job, const uint16_t* q, long long q_stride, int G, int wave, int lane) {
+    constexpr int D = kHeadDim;
+    const int col = lane & 31;
+    half = lane >> 5;
+    my = min(32 * wave + col, job.rows - 1);
+    const int tok = job.token_of(my, G);
+    my_end = min(job.s1, job.pos0 + tok + 1);
+    all = min(job.s1, job.pos0 + job.token_of(min(32 * wave, job.rows - 1), G) + 1);
+    const uint16_t* p = q + (long long)(job.row0 + tok) * q_stride + (long long)(job.h * G + (job.qt * TR + my) - tok * G) * D + 8 * half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) qb[i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(p + 16 * i));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) oc[i] = f32x16_t{};
+    m_run = kNegBig;
+    l_run = 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) k_at[s] = col * 256 + (((2 * s + half) ^ swz_k(col)) << 4);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const int r = 4 * half + ((lane & 15) >> 2), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      v_at[d] = r * 256 + ((c ^ swz_v(r)) << 4) + 8 * (lane & 1);
+    }
+  }
+  // logits of 32 tokens of K at kt
+  __device__ __forceinline__ f32x16_t logits(lds_ptr kt) const {
+    f32x16_t sv = {};
 #pragma unroll
     for (int s = 0; s < 8; ++s)
-      sv = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t*)(k_at[s] + at)), qb[s], s == 0 ? f32x16_t{} : sv, 0, 0, 0);
-  };
-  auto output = [&](int at, const Weights& p) FASA_INLINE {
+      sv = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t*)(kt + k_at[s])), qb[s], sv, 0, 0, 0);
+    return sv;
+  }
+  // the weighted 32 tokens of V at vt
+  __device__ __forceinline__ void output(lds_ptr vt, const Weights& p) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const lds_ptr from = v_at[d] + (at + s * 16 * 256);
+        const lds_ptr from = vt + v_at[d] + s * 16 * 256;
         const uint2 lo = lds_read_tr(from), hi = lds_read_tr(from + 8 * 256);            // (rows r and r + 8 have the same swizzle)
         oc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(lo.x, lo.y, hi.x, hi.y)),
                                                         __builtin_bit_cast(bf16x8_t, make_uint4(p.w[4 * s], p.w[4 * s + 1], p.w[4 * s + 2], p.w[4 * s + 3])), oc[d], 0, 0, 0);
       }
-  };
-  auto by_scale = [&](f32x16_t& sv, const float* f) FASA_INLINE {
+  }
+  __device__ __forceinline__ void by_scale(f32x16_t& sv, const float* f) const {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const float4 x = *reinterpret_cast<const float4*>(f + 8 * g + 4 * half);
       sv[4 * g] *= x.x; sv[4 * g + 1] *= x.y; sv[4 * g + 2] *= x.z; sv[4 * g + 3] *= x.w;
     }
-  };
-  // Weights of logits sv (tokens n0 .. n0 + 31); by: the factor by which the running sums go down.
-  auto softmax = [&](f32x16_t& sv, Weights& p, float& by, int n0, const float* ks, const float* vs) FASA_INLINE {
+  }
+  // Weights of logits sv (tokens n0 .. n0 + 31; 8-bit: ks, vs their scales, ks with the softmax's), and the factor by which the running sums go down.
+  __device__ __forceinline__ float softmax(f32x16_t& sv, Weights& p, int n0, const float* ks, const float* vs, float scale_log2e) {
     if constexpr (BYTES) by_scale(sv, ks);
-    if (n0 + 32 > wave_all) {
+    if (n0 + 32 > all) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sv[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < my_end ? sv[i] : kNegBig;
     }
-    float mx = xor32_max(largest(sv));
+    float mx = __builtin_fmaxf(sv[0], sv[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) mx = __builtin_fmaxf(mx, __builtin_fmaxf(sv[i], sv[i + 1]));
+    mx = xor32_max(mx);
     if constexpr (!BYTES) mx *= scale_log2e;
-    const float m_new = fmaxf(m_run, mx);
-    by = __builtin_amdgcn_exp2f(m_run - m_new);
+    const float m_new = __builtin_fmaxf(m_run, mx), by = __builtin_amdgcn_exp2f(m_run - m_new);
     m_run = m_new;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sv[i] = __builtin_amdgcn_exp2f(BYTES ? sv[i] - m_new : __builtin_fmaf(sv[i], scale_log2e, -m_new));
@@ -427,7 +243,7 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) p.w[i] = pack_bf16(sv[2 * i], sv[2 * i + 1]);
-    if constexpr (!BYTES) {                                // the sum of the weights as the product has them: two at a time
+    if constexpr (!BYTES) {                                // the sum of the weights as the product has them, two at a time
       const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
       float other = 0.f;
 #pragma unroll
@@ -437,92 +253,190 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
       }
       l_run += other;
     }
-  };
-  // step: logits of the next 32 tokens -> nxt, output of the ones before (pp), weights of these (cur -> pc)
-  auto step = [&](f32x16_t& cur, f32x16_t& nxt, const Weights& pp, Weights& pc, int k_next, int v_last, int n0, const float* ks, const float* vs) FASA_INLINE {
-    float by;
-    logits(k_next, nxt);
-    output(v_last, pp);
-    softmax(cur, pc, by, n0, ks, vs);
-    if (__ballot(by != 1.f) != 0ull) {
-#pragma unroll
-      for (int d = 0; d < 4; ++d) oc[d] *= by;
-    }
-  };
-
-  if (n_tiles > 0) {
-    f32x16_t sa, sb;
-    Weights pa = {}, pb;
-    const auto of_k = [](int r) { return swz_k(r); };
-    const auto of_v = [](int r) { return swz_v(r); };
-    float rsk = 0.f, rsv = 0.f;
-    // K of tiles 0 and 1, V of tile 0; zeros for V of the tile before the first, which has no weights, but what 0 is multiplied by has to be a number
-    Rows ra = rows_of(s0, look_up(s0)), rb = rows_of(s0 + kWideTok, look_up(s0 + kWideTok)), rc = rows_of(s0 + 2 * kWideTok, look_up(s0 + 2 * kWideTok));
-    store_rows(smk, load_rows(Kh, ra), of_k);
-    store_rows(smv, load_rows(Vh, ra), of_v);
-    store_rows(smk + kTileBytes, load_rows(Kh, rb), of_k);
-    if constexpr (BYTES) {
-      ssk[lane] = load_scale(ks_h, s0, ra) * scale_log2e;                               // (all waves, the same)
-      ssv[lane] = load_scale(vs_h, s0, ra);
-      ssk[kWideTok + lane] = load_scale(ks_h, s0 + kWideTok, rb) * scale_log2e;
-      rsk = load_scale(ks_h, s0 + 2 * kWideTok, rc);
-    }
-    for (int x = t; x < kTileBytes / 16; x += NT) reinterpret_cast<uint4*>(smv + (kDeepSlots - 1) * kTileBytes)[x] = make_uint4(0, 0, 0, 0);
-    u32xl raw = load_rows(Kh, rc);
-    int blks = look_up(s0 + 3 * kWideTok);
-    __syncthreads();
-    logits(0, sa);
-    // Tile T, in slot c0 (c1, c2: slots of T + 1 and T + 2, the latter T - 1's too).  Before it: raw is K of tile T + 2, r1 and r2 are the rows of T + 1 and T + 2,
-    // blks the blocks of T + 3, whose rows r0 becomes.
-    auto tile = [&](int T, int c0, int c1, int c2, Rows& r0, const Rows& r1) FASA_INLINE {
-      constexpr int B = kTileBytes;
-      const int j0 = s0 + T * kWideTok;
-      store_rows(smk + c2 * B, raw, of_k);
-      raw = load_rows(Vh, r1);
-      if constexpr (BYTES) {
-        ssk[c2 * kWideTok + lane] = rsk * scale_log2e;
-        rsv = load_scale(vs_h, j0 + kWideTok, r1);
-      }
-      step(sa, sb, pa, pb, c0 * B + 32 * 256, c2 * B + 32 * 256, j0, ssk + c0 * kWideTok, ssv + c0 * kWideTok);
-      store_rows(smv + c1 * B, raw, of_v);
-      r0 = rows_of(j0 + 3 * kWideTok, blks);
-      raw = load_rows(Kh, r0);
-      if constexpr (BYTES) {
-        ssv[c1 * kWideTok + lane] = rsv;
-        rsk = load_scale(ks_h, j0 + 3 * kWideTok, r0);
-      }
-      blks = look_up(j0 + 4 * kWideTok);
-      step(sb, sa, pb, pa, c1 * B, c0 * B, j0 + 32, ssk + c0 * kWideTok + 32, ssv + c0 * kWideTok + 32);
-      __syncthreads();
-    };
-    int c0 = 0, c1 = 1, c2 = 2;
-    for (int T = 0; T < n_tiles; ++T) {
-      tile(T, c0, c1, c2, ra, rb);
-      const Rows r = ra; ra = rb; rb = rc; rc = r;
-      const int c = c0; c0 = c1; c1 = c2; c2 = c;
-    }
-    output(c2 * kTileBytes + 32 * 256, pa);
+    return by;
   }
-  l_run = xor32_sum(l_run);
-  if (32 * wave + col >= rows) return;
-  if (splits == 1) {
-    const float by = 1.0f / l_run;
-    uint16_t* o = O + (long long)(sc.row + my_tok) * o_stride + (long long)(h * G + (qt * TR + my) - my_tok * G) * D + 4 * half;
+  __device__ __forceinline__ void rescale(float by) {
+    if (__ballot(by != 1.f) == 0ull) return;               // (after the first tiles a new maximum is rare)
+#pragma unroll
+    for (int d = 0; d < 4; ++d) oc[d] *= by;
+  }
+  // To O, or where there are splits to their places.  row: of the tile, before it was clamped.
+  template <int TR>
+  __device__ __forceinline__ void finish(const WideJob<TR>& job, int row, uint16_t* O, long long o_stride, int G, float* part_acc, float2* part_ml, int Hkv, int tiles_each, int splits) {
+    constexpr int D = kHeadDim;
+    const float l = xor32_sum(l_run);
+    if (row >= job.rows) return;
+    if (splits == 1) {
+      const float by = 1.0f / l;
+      const int tok = job.token_of(my, G);
+      uint16_t* o = O + (long long)(job.row0 + tok) * o_stride + (long long)(job.h * G + (job.qt * TR + my) - tok * G) * D + 4 * half;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<uint2*>(o + 32 * d + 8 * g) = make_uint2(pack_bf16(oc[d][4 * g] * by, oc[d][4 * g + 1] * by), pack_bf16(oc[d][4 * g + 2] * by, oc[d][4 * g + 3] * by));
+      return;
+    }
+    const size_t to = (((size_t)(job.b * Hkv + job.h) * tiles_each + job.qt) * splits + job.split) * TR + my;
+    float* pa = part_acc + to * D + 4 * half;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<uint2*>(o + 32 * d + 8 * g) = make_uint2(pack_bf16(oc[d][4 * g] * by, oc[d][4 * g + 1] * by), pack_bf16(oc[d][4 * g + 2] * by, oc[d][4 * g + 3] * by));
-    return;
+        *reinterpret_cast<float4*>(pa + 32 * d + 8 * g) = make_float4(oc[d][4 * g], oc[d][4 * g + 1], oc[d][4 * g + 2], oc[d][4 * g + 3]);
+    if (half == 0) part_ml[to] = make_float2(m_run, l);
   }
-  const size_t at = (((size_t)(b * Hkv + h) * tiles_each + qt) * splits + split) * TR + my;
-  float* to = part_acc + at * D + 4 * half;
+};
+
+// Few query rows (up to 128 of a KV head): bound by reading the rows, which four waves share; two workgroups a compute unit have 64 KB of loads in flight.
+constexpr int kShortWaves = 4, kShortRows = 32 * kShortWaves;
+template <CacheFmt F, bool APART>
+__global__ __launch_bounds__(64 * kShortWaves, 2) void chunk_short_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
+                                                                         uint16_t* __restrict__ O, float* __restrict__ part_acc,
+                                                                         float2* __restrict__ part_ml, CacheView cv, ChunkView ch, int batch, int Hkv,
+                                                                         int G, int tiles_each, int splits, long long q_stride, long long o_stride,
+                                                                         float scale_log2e) {
+  constexpr bool BYTES = F != kPlain;
+  extern __shared__ __align__(16) unsigned char smem[];    // [2][K tile, V tile], then scales [2][k 64, v 64]
+  float* const sm_scale = reinterpret_cast<float*>(smem + 4 * kTileBytes);
+  WideJob<kShortRows> job;
+  if (!job.find(ch, batch, Hkv, G, tiles_each, splits)) return;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  using Loader = WideLoader<F, kShortWaves, APART>;
+  const Loader ld(cv, K, V, q, job.b, job.h, job.s1, wave, lane);
+  WideQueries<BYTES> wq(job, q, q_stride, G, wave, lane);
+  const bool mine = 32 * wave < job.rows;                  // waves without a row only load
+  if (job.n_tiles > 0) {
+    typename Loader::u32xl rk, rv;
+    float sk = 0.f, sv = 0.f;
+    int next = ld.look_up(job.s0);                         // of the tile to be loaded next
+    auto load = [&](int j0) FASA_INLINE {
+      const typename Loader::Rows r = ld.rows_of(j0, next);
+      rk = ld.load(ld.Kh, r);
+      rv = ld.load(ld.Vh, r);
+      if constexpr (BYTES) {
+        sk = ld.load_scale(ld.ks, j0, r);
+        sv = ld.load_scale(ld.vs, j0, r);
+      }
+      next = ld.look_up(j0 + kWideTok);
+    };
+    auto store = [&](int buf) FASA_INLINE {
+      ld.store_k(smem + buf * 2 * kTileBytes, rk);
+      ld.store_v(smem + buf * 2 * kTileBytes + kTileBytes, rv);
+      if constexpr (BYTES) {                               // (all waves, the same)
+        sm_scale[buf * 2 * kWideTok + lane] = sk * scale_log2e;
+        sm_scale[buf * 2 * kWideTok + kWideTok + lane] = sv;
+      }
+    };
+    load(job.s0);
+    store(0);
+    load(job.s0 + kWideTok);
+    __syncthreads();
+    for (int T = 0; T < job.n_tiles; ++T) {
+      const int j0 = job.s0 + T * kWideTok, buf = T & 1;
+      store(buf ^ 1);                                      // tile T + 1; behind the last: the last row, for nobody
+      load(j0 + 2 * kWideTok);
+      if (mine) {
+        const lds_ptr kt = (lds_ptr)smem + buf * 2 * kTileBytes;
+        const float* ks = sm_scale + buf * 2 * kWideTok;
+        f32x16_t s[2];
+        typename WideQueries<BYTES>::Weights p;
+        s[0] = wq.logits(kt);
+        s[1] = wq.logits(kt + 32 * 256);
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<float4*>(to + 32 * d + 8 * g) = make_float4(oc[d][4 * g], oc[d][4 * g + 1], oc[d][4 * g + 2], oc[d][4 * g + 3]);
-  if (half == 0) part_ml[at] = make_float2(m_run, l_run);
+        for (int i = 0; i < 2; ++i) {
+          wq.rescale(wq.softmax(s[i], p, j0 + 32 * i, ks + 32 * i, ks + kWideTok + 32 * i, scale_log2e));
+          wq.output(kt + kTileBytes + i * 32 * 256, p);
+        }
+      }
+      __syncthreads();
+    }
+  }
+  wq.finish(job, 32 * wave + (lane & 31), O, o_stride, G, part_acc, part_ml, Hkv, tiles_each, splits);
+}
+
+// Many: eight waves (256 rows a tile), two a SIMD.  In steps of 32 tokens: step u runs the logits of step u + 1 and the output of step u - 1 ahead of its own
+// softmax, so that the matrix cores have sixteen products in a row to do that wait for nothing.
+constexpr int kDeepWaves = 8, kDeepRows = 32 * kDeepWaves;
+constexpr int kDeepSlots = 3;                             // tiles of K, and of V, in LDS: K of tiles T, T + 1 and V of T - 1, T are read while K of T + 2 and V of T + 1 are written
+template <CacheFmt F>
+__global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
+                                                                       uint16_t* __restrict__ O, float* __restrict__ part_acc,
+                                                                       float2* __restrict__ part_ml, CacheView cv, ChunkView ch, int batch, int Hkv,
+                                                                       int G, int tiles_each, int splits, long long q_stride, long long o_stride,
+                                                                       float scale_log2e) {
+  constexpr int NT = 64 * kDeepWaves, B = kTileBytes;
+  constexpr bool BYTES = F != kPlain;
+  extern __shared__ __align__(16) unsigned char smem[];   // [slot] K tiles, [slot] V tiles, then scales [slot][k 64], [slot][v 64]
+  unsigned char* const smk = smem;
+  unsigned char* const smv = smem + kDeepSlots * B;
+  float* const ssk = reinterpret_cast<float*>(smem + 2 * kDeepSlots * B);
+  float* const ssv = ssk + kDeepSlots * kWideTok;
+  WideJob<kDeepRows> job;
+  if (!job.find(ch, batch, Hkv, G, tiles_each, splits)) return;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  using Loader = WideLoader<F, kDeepWaves, false>;
+  using Rows = typename Loader::Rows;
+  const Loader ld(cv, K, V, q, job.b, job.h, job.s1, wave, lane);
+  WideQueries<BYTES> wq(job, q, q_stride, G, wave, lane);
+  using Weights = typename WideQueries<BYTES>::Weights;
+  const int s0 = job.s0;
+  // step: logits of the next 32 tokens -> nxt, output of the ones before (pp), weights of these (cur -> pc)
+  auto step = [&](f32x16_t& cur, f32x16_t& nxt, const Weights& pp, Weights& pc, int k_next, int v_last, int n0, const float* ks, const float* vs) FASA_INLINE {
+    nxt = wq.logits((lds_ptr)smk + k_next);
+    wq.output((lds_ptr)smv + v_last, pp);
+    wq.rescale(wq.softmax(cur, pc, n0, ks, vs, scale_log2e));
+  };
+  if (job.n_tiles > 0) {
+    f32x16_t sa, sb;
+    Weights pa = {}, pb;
+    float rsk = 0.f, rsv = 0.f;
+    // K of tiles 0 and 1, V of tile 0; zeros for V of the tile before the first, which has no weights, but what 0 is multiplied by has to be a number
+    const int e0 = ld.look_up(s0), e1 = ld.look_up(s0 + kWideTok), e2 = ld.look_up(s0 + 2 * kWideTok);
+    Rows ra = ld.rows_of(s0, e0), rb = ld.rows_of(s0 + kWideTok, e1), rc = ld.rows_of(s0 + 2 * kWideTok, e2);
+    const auto k0 = ld.load(ld.Kh, ra), v0 = ld.load(ld.Vh, ra), k1 = ld.load(ld.Kh, rb);
+    auto raw = ld.load(ld.Kh, rc);
+    int entry = ld.look_up(s0 + 3 * kWideTok);
+    ld.store_k(smk, k0);
+    ld.store_v(smv, v0);
+    ld.store_k(smk + B, k1);
+    if constexpr (BYTES) {
+      ssk[lane] = ld.load_scale(ld.ks, s0, ra) * scale_log2e;                             // (all waves, the same)
+      ssv[lane] = ld.load_scale(ld.vs, s0, ra);
+      ssk[kWideTok + lane] = ld.load_scale(ld.ks, s0 + kWideTok, rb) * scale_log2e;
+      rsk = ld.load_scale(ld.ks, s0 + 2 * kWideTok, rc);
+    }
+    for (int x = t; x < B / 16; x += NT) reinterpret_cast<uint4*>(smv + (kDeepSlots - 1) * B)[x] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    sa = wq.logits((lds_ptr)smk);
+    // Tile T in slot c0; c1, c2: slots of T + 1 and T + 2, the latter T - 1's too.  Before it: raw is K of tile T + 2, rb and rc are the rows of T + 1 and T + 2,
+    // entry of T + 3.  (Every wave runs all tiles, for the barriers.)
+    int c0 = 0, c1 = 1, c2 = 2;
+    for (int T = 0; T < job.n_tiles; ++T) {
+      const int j0 = s0 + T * kWideTok;
+      ld.store_k(smk + c2 * B, raw);
+      raw = ld.load(ld.Vh, rb);
+      if constexpr (BYTES) {
+        ssk[c2 * kWideTok + lane] = rsk * scale_log2e;
+        rsv = ld.load_scale(ld.vs, j0 + kWideTok, rb);
+      }
+      step(sa, sb, pa, pb, c0 * B + 32 * 256, c2 * B + 32 * 256, j0, ssk + c0 * kWideTok, ssv + c0 * kWideTok);
+      ld.store_v(smv + c1 * B, raw);
+      rb = rc;
+      rc = ld.rows_of(j0 + 3 * kWideTok, entry);
+      raw = ld.load(ld.Kh, rc);
+      if constexpr (BYTES) {
+        ssv[c1 * kWideTok + lane] = rsv;
+        rsk = ld.load_scale(ld.ks, j0 + 3 * kWideTok, rc);
+      }
+      entry = ld.look_up(j0 + 4 * kWideTok);
+      step(sb, sa, pb, pa, c1 * B, c0 * B, j0 + 32, ssk + c0 * kWideTok + 32, ssv + c0 * kWideTok + 32);
+      __syncthreads();
+      const int c = c0; c0 = c1; c1 = c2; c2 = c;
+    }
+    wq.output((lds_ptr)smv + c2 * B + 32 * 256, pa);
+  }
+  wq.finish(job, 32 * wave + (lane & 31), O, o_stride, G, part_acc, part_ml, Hkv, tiles_each, splits);
 }
 
 // Joins the splits of a tile's rows: 32 lanes a row, four dims each.
@@ -554,39 +468,45 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restric
       make_uint2(pack_bf16(a.x * by, a.y * by), pack_bf16(a.z * by, a.w * by));
 }
 
-template <CacheFmt F, int NW>
-static hipError_t wide_t(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
-  using RT = typename RowType<uint16_t, F>::type;
+template <int TR, class Kernel>
+static hipError_t wide_t(Kernel kernel, size_t lds, const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
   const int hkv = s.n_kv_heads, G = s.n_q_heads / hkv;
-  hipError_t e = launch_lds("fasa_chunk_attend", chunk_wide_kernel<F, NW>, dim3((unsigned)((long long)p.tiles * hkv * p.splits)), dim3(64 * NW),
-                            4 * kTileBytes + (F == kPlain ? 0 : 4 * kWideTok * 4), st, (const uint16_t*)a.q, (const RT*)a.cv.K, (const RT*)a.cv.V,
-                            (uint16_t*)a.O, a.part_acc, (float2*)a.part_ml, a.cv, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.q_stride, a.o_stride,
-                            1.4426950408889634f / sqrtf((float)s.head_dim));
+  const hipError_t e = launch_lds("fasa_chunk_attend", kernel, dim3((unsigned)((long long)p.tiles * hkv * p.splits)), dim3(2 * TR), lds, st, (const uint16_t*)a.q,
+                                  (const void*)a.cv.K, (const void*)a.cv.V, (uint16_t*)a.O, a.part_acc, (float2*)a.part_ml, a.cv, a.ch, s.batch, hkv, G,
+                                  p.per_seq, p.splits, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
   if (e != hipSuccess || p.splits == 1) return e;
-  return launch("fasa_chunk_merge", chunk_merge_kernel<32 * NW>, dim3((unsigned)p.tiles * 4 * NW, hkv), dim3(256), st, (const float*)a.part_acc,
+  return launch("fasa_chunk_merge", chunk_merge_kernel<TR>, dim3((unsigned)p.tiles * (TR / 8), hkv), dim3(256), st, (const float*)a.part_acc,
                 (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.o_stride);
 }
-
-template <CacheFmt F> static hipError_t deep_t(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
-  using RT = typename RowType<uint16_t, F>::type;
-  const int hkv = s.n_kv_heads, G = s.n_q_heads / hkv;
-  const hipError_t e = launch_lds("fasa_chunk_attend", chunk_deep_kernel<F>, dim3((unsigned)((long long)p.tiles * hkv * p.splits)), dim3(64 * kDeepWaves),
-                                  2 * kDeepSlots * (kTileBytes + (F == kPlain ? 0 : kWideTok * 4)), st, (const uint16_t*)a.q, (const RT*)a.cv.K, (const RT*)a.cv.V,
-                                  (uint16_t*)a.O, a.part_acc, (float2*)a.part_ml, a.cv, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.q_stride, a.o_stride,
-                                  1.4426950408889634f / sqrtf((float)s.head_dim));
-  if (e != hipSuccess || p.splits == 1) return e;
-  return launch("fasa_chunk_merge", chunk_merge_kernel<kDeepRows>, dim3((unsigned)p.tiles * (kDeepRows / 8), hkv), dim3(256), st, (const float*)a.part_acc,
-                (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.o_stride);
+template <CacheFmt F> static hipError_t wide_f(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
+  const size_t scales = F == kPlain ? 0 : kWideTok * 4;
+  if (p.tile_rows == kDeepRows) return wide_t<kDeepRows>(chunk_deep_kernel<F>, 2 * kDeepSlots * (kTileBytes + scales), s, p, a, st);
+  return wide_t<kShortRows>(p.apart ? chunk_short_kernel<F, true> : chunk_short_kernel<F, false>, 4 * (kTileBytes + scales), s, p, a, st);
 }
-
 hipError_t launch_chunk_wide(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
-  if (p.tile_rows == 128)
-    return a.fmt == kPlain ? wide_t<kPlain, 4>(s, p, a, st) : a.fmt == kInt8 ? wide_t<kInt8, 4>(s, p, a, st) : wide_t<kE4m3, 4>(s, p, a, st);
-  // pages of fewer tokens than a wave's load has rows, or rows far apart: tokens are looked up one by one
-  const bool apart = (a.cv.pm.table != nullptr && (1 << a.cv.pm.shift) < (a.fmt == kPlain ? 4 : 8)) ||
-                     a.cv.sn >= (1ll << 27) || a.cv.sb >= (1ll << 31);
-  if (apart) return a.fmt == kPlain ? wide_t<kPlain, 8>(s, p, a, st) : a.fmt == kInt8 ? wide_t<kInt8, 8>(s, p, a, st) : wide_t<kE4m3, 8>(s, p, a, st);
-  return a.fmt == kPlain ? deep_t<kPlain>(s, p, a, st) : a.fmt == kInt8 ? deep_t<kInt8>(s, p, a, st) : deep_t<kE4m3>(s, p, a, st);
+  return a.fmt == kPlain ? wide_f<kPlain>(s, p, a, st) : a.fmt == kInt8 ? wide_f<kInt8>(s, p, a, st) : wide_f<kE4m3>(s, p, a, st);
+}
+
+// Rows of 256, of 128 where a KV head has no more or where rows have to be looked up one by one.  Splits: as many as fill the compute units once (128: two
+// workgroups a compute unit), of 256 tokens or more.
+ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start) {
+  ChunkPlan p{};
+  const int G = s.n_q_heads / s.n_kv_heads;
+  const long long m = (long long)n_new * G;
+  p.wide = true;
+  p.apart = apart;
+  p.tile_rows = m <= kShortRows || apart ? kShortRows : kDeepRows;
+  p.tiles = (int)chunk_tiles(by_row_start, s.batch, n_new, n_rows, G, p.tile_rows);
+  p.per_seq = (int)((m + p.tile_rows - 1) / p.tile_rows);
+  long long n = kAssumedCUs * (p.tile_rows == kShortRows ? 2 : 1) / ((long long)p.tiles * s.n_kv_heads);
+  const int most = (s.n_ctx + 255) / 256;
+  if (n > most) n = most;
+  if (n > 64) n = 64;
+  p.splits = n < 1 ? 1 : (int)n;
+  const size_t parts = p.splits == 1 ? 0 : (size_t)s.batch * s.n_kv_heads * p.per_seq * p.splits * p.tile_rows;
+  p.part_acc_bytes = parts * kHeadDim * 4;
+  p.part_ml_bytes = parts * 8;
+  return p;
 }
 
 }  // namespace fasa
