@@ -161,7 +161,7 @@ template <bool BYTES> struct WideQueries {
   struct Weights { uint32_t w[8]; };                       // of 32 tokens
   bf16x8_t qb[8];
   f32x16_t oc[4];
-  float m_run, l_run;                                      // of this lane's query (log2 domain); l_run over this lane's tokens
+  float m_run, l_run;                                      // of this lane's query: what the weights are relative to (log2 domain), their sum over this lane's tokens
   uint32_t k_at[8], v_at[4];                               // places of this lane's operands in a tile, of its first 32 (16) tokens
   int my, my_end, all, half;                               // row in the tile, tokens that it sees, tokens that all rows of the wave see
   long long at;                                            // of the row, in elements of q
@@ -217,8 +217,10 @@ template <bool BYTES> struct WideQueries {
       sv[4 * g] *= x.x; sv[4 * g + 1] *= x.y; sv[4 * g + 2] *= x.z; sv[4 * g + 3] *= x.w;
     }
   }
-  // Weights of logits sv (tokens n0 .. n0 + 31; 8-bit: ks, vs their scales, ks with the softmax's), and the factor by which the running sums go down.
-  __device__ __forceinline__ float softmax(f32x16_t& sv, Weights& p, int n0, const float* ks, const float* vs, float scale_log2e) {
+  // Weights of logits sv (tokens n0 .. n0 + 31; 8-bit: ks, vs their scales, ks with the softmax's).  What they are relative to follows the running maximum only
+  // where that has grown by more than 2^8 (weights of up to 256 are as exact as those below 1): with 32 queries a wave, one of them has a new maximum in every
+  // step of the first 32, and in 32 / u of the steps u behind, and 64 accumulators would be multiplied there.
+  __device__ __forceinline__ void softmax(f32x16_t& sv, Weights& p, int n0, const float* ks, const float* vs, float scale_log2e) {
     if constexpr (BYTES) by_scale(sv, ks);
     if (n0 + 32 > all) {
 #pragma unroll
@@ -229,11 +231,15 @@ template <bool BYTES> struct WideQueries {
     for (int i = 2; i < 16; i += 2) mx = __builtin_fmaxf(mx, __builtin_fmaxf(sv[i], sv[i + 1]));
     mx = xor32_max(mx);
     if constexpr (!BYTES) mx *= scale_log2e;
-    const float m_new = __builtin_fmaxf(m_run, mx), by = __builtin_amdgcn_exp2f(m_run - m_new);
-    m_run = m_new;
+    if (__ballot(mx > m_run + 8.f) != 0ull) {
+      const float m_new = __builtin_fmaxf(m_run, mx), by = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= by;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sv[i] = __builtin_amdgcn_exp2f(BYTES ? sv[i] - m_new : __builtin_fmaf(sv[i], scale_log2e, -m_new));
-    l_run *= by;
+      for (int d = 0; d < 4; ++d) oc[d] *= by;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sv[i] = __builtin_amdgcn_exp2f(BYTES ? sv[i] - m_run : __builtin_fmaf(sv[i], scale_log2e, -m_run));
     if constexpr (BYTES) {
       float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -253,12 +259,6 @@ template <bool BYTES> struct WideQueries {
       }
       l_run += other;
     }
-    return by;
-  }
-  __device__ __forceinline__ void rescale(float by) {
-    if (__ballot(by != 1.f) == 0ull) return;               // (after the first tiles a new maximum is rare)
-#pragma unroll
-    for (int d = 0; d < 4; ++d) oc[d] *= by;
   }
   // To O, or where there are splits to their places.  row: of the tile, before it was clamped.
   template <int TR>
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void chunk_short_kernel(const 
         s[1] = wq.logits(kt + 32 * 256);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          wq.rescale(wq.softmax(s[i], p, j0 + 32 * i, ks + 32 * i, ks + kWideTok + 32 * i, scale_log2e));
+          wq.softmax(s[i], p, j0 + 32 * i, ks + 32 * i, ks + kWideTok + 32 * i, scale_log2e);
           wq.output(kt + kTileBytes + i * 32 * 256, p);
         }
       }
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
   auto step = [&](f32x16_t& cur, f32x16_t& nxt, const Weights& pp, Weights& pc, int k_next, int v_last, int n0, const float* ks, const float* vs) FASA_INLINE {
     nxt = wq.logits((lds_ptr)smk + k_next);
     wq.output((lds_ptr)smv + v_last, pp);
-    wq.rescale(wq.softmax(cur, pc, n0, ks, vs, scale_log2e));
+    wq.softmax(cur, pc, n0, ks, vs, scale_log2e);
   };
   if (job.n_tiles > 0) {
     f32x16_t sa, sb;
