@@ -516,7 +516,7 @@ struct ChunkLayout {
 // The part of the workspace that has to be zero comes first, where the other calls have it; the partial results behind it.
 ChunkLayout chunk_layout(fasa_shape s, const ChunkView& ch, bool apart) {
   ChunkLayout L;
-  L.plan = plan_chunk(s, apart, ch.n_new, ch.n_rows, ch.row_start != nullptr);
+  L.plan = plan_chunk(s, apart, ch);
   s.budget = s.n_ctx;                     // (any: that part does not depend on it)
   const WsLayout w = ws_layout(s);
   L.acc_off = w.cand_off;

@@ -1,15 +1,26 @@
 // Attention of a few query rows of a KV head over its cache: single tokens, a few drafted ones, and float32 chunks of any length.
 // Query rows (new token i, head g of the group) of a sequence and KV head go by tiles of 16, the columns of the matrix cores' 16-row
-// tile engine (mfma_tile.h); a tile's tokens are shared out to `splits` workgroups of eight waves, a wave takes 16 at a time, and the
-// last workgroup of a tile by ticket merges the partial results.  Bound by reading the rows, once per tile: 2 d bytes e a token.
+// tile engine (mfma_tile.h); a tile's tokens are shared out to workgroups, a wave of which takes 16 at a time, and the
+// last workgroup of a tile by ticket merges the partial results.  Bound by reading the rows, once per tile.
+#include <algorithm>
+
 #include "chunk_common.h"
 #include "mfma_tile.h"
 
 namespace fasa {
 
-constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / kWave;
+// Waves of a workgroup.  A wave has a tile of 16 tokens in flight: 8 KB of bf16 rows, 4 KB of 8-bit ones, of which a compute unit needs eight for what four of the former
+// do.  us, four / eight waves: bf16, 8 rows of 8192: 12.0 / 13.0, of 32768: 29.9 / 31.8, 128 of 4864 - 16384: 134 / 138; e4m3, 8 of 131072: 69.8 / 52.4 (with two tiles in
+// flight 58.0); float32, 37 new tokens over 4096: 18.2 / 15.9.
+template <typename ET, CacheFmt F> constexpr int kChunkWaves = F == kPlain && sizeof(ET) == 2 ? 4 : 8;
 constexpr int kChunkRows = 16;                           // query rows of a tile
-constexpr int kChunkStep = 16 * kChunkWaves;             // tokens of a round of the waves
+constexpr int kChunkLeast = 64;                          // tokens of a part, at least
+constexpr int kChunkSplits = 256;                        // parts of a tile, at most
+// Workgroups of a call whose tiles are split, at most; twice as many where sequences differ in length, whose shares may then be more alike (128 rows of 4864 - 16384,
+// int8: 89 / 86 us, e4m3 88 / 84).
+constexpr int kChunkResident = kAssumedCUs;
+constexpr int kTicketWords = 8;                          // from a tile's ticket to the next: tickets of different rows, whose workgroups run on different XCDs, share no line
+static_assert(2 * kChunkResident * kTicketWords <= kChunkTickets, "a ticket for each tile");
 
 // One lane's share of 16 rows as stored; K: chunks hi, hi + 4, .. of 16 bytes of row lo, V: dims 8lo .. 8lo + 7 of rows 4hi .. 4hi + 3
 template <typename ET, CacheFmt F> struct RawKV {
@@ -55,153 +66,170 @@ template <typename ET, CacheFmt F> __device__ __forceinline__ int chunk_dim(int 
 
 // SMALL: pages of fewer than 16 tokens, whose rows are looked up one by one; else the 16 rows of a tile lie in one block.
 template <typename ET, CacheFmt F, bool SMALL>
-__global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __restrict__ q, const typename RowType<ET, F>::type* __restrict__ K,
-                                                                 const typename RowType<ET, F>::type* __restrict__ V, ET* __restrict__ O,
-                                                                 float* __restrict__ part_acc, float* __restrict__ part_ml,
-                                                                 uint32_t* __restrict__ tickets, CacheView cv, ChunkView ch, int batch, int Hkv,
-                                                                 int G, int tiles_each, int splits, int cap, long long q_stride,
-                                                                 long long o_stride, float scale_log2e) {
-  constexpr int D = kHeadDim;
+__global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
+    const ET* __restrict__ q, const typename RowType<ET, F>::type* __restrict__ K, const typename RowType<ET, F>::type* __restrict__ V, ET* __restrict__ O,
+    float* __restrict__ part_acc, float2* __restrict__ part_ml, uint32_t* __restrict__ tickets, CacheView cv, ChunkView ch, int batch, int Hkv, int G,
+    int tiles_each, int all_splits, int units, int all_units, int cap, long long q_stride, long long o_stride, float scale_log2e) {
+  constexpr int D = kHeadDim, NWV = kChunkWaves<ET, F>, NT = 64 * NWV, ROUND = 16 * NWV;     // tokens of a round of the waves
   constexpr bool F32 = sizeof(ET) == 4;
   using RT = typename RowType<ET, F>::type;
-  // waves' totals: [wave][cap][D], then m, l [wave][cap]; the merge: weights [split][cap], then the partitions' sums
+  // waves' totals: [wave][cap][D], then m, l [wave][cap]; the merge: weights [row][split]
   extern __shared__ __align__(16) float lds[];
-  __shared__ __align__(16) float scs[kChunkWaves][16];
+  __shared__ __align__(16) float scs[NWV][16];
   __shared__ float red[kChunkRows];
   __shared__ uint32_t ticket;
 
-  // workgroups: heads fastest (the blocks of a paged cache often hold all heads' rows side by side), then splits
-  unsigned id = blockIdx.x;
-  const int h = (int)(id % (unsigned)Hkv);
-  id /= (unsigned)Hkv;
-  const int split = (int)(id % (unsigned)splits);
-  id /= (unsigned)splits;
-  int b, qt;
-  if (!find_chunk_tile<kChunkRows>(ch, batch, G, tiles_each, id, b, qt)) return;
-  const SeqChunk sc = seq_chunk(ch, b);
-  const int rows = min(cap, sc.n_new * G - qt * kChunkRows);        // of this tile
-  if (rows <= 0) return;
+  // workgroups: heads fastest (the blocks of a paged cache often hold all heads' rows side by side)
+  const int h = (int)(blockIdx.x % (unsigned)Hkv);
+  ChunkUnit u;
+  if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, all_splits, units, kChunkLeast, blockIdx.x / (unsigned)Hkv, u)) return;
+  const int b = u.b, splits = u.splits, qrow = u.tile * kChunkRows;
+  const int rows = min(cap, u.seq.n_new * G - qrow);                 // of this tile
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int lo = lane & 15, hi = lane >> 4;
-  const int pos0 = sc.n_ctx - sc.n_new;
-  const auto token_of = [&](int r) FASA_INLINE { return (qt * kChunkRows + r) / G; };
-  // tokens [0, seen) are seen by the last row of the tile
-  const int seen = pos0 + token_of(rows - 1) + 1;
-  const int share = ((seen + splits - 1) / splits + 15) & ~15;
-  const int s0 = min(split * share, seen), s1 = min(seen, s0 + share);
+  const int pos0 = u.seq.n_ctx - u.seq.n_new;
+  const auto token_of = [&](int r) FASA_INLINE { return (qrow + r) / G; };
+  const int seen = pos0 + token_of(rows - 1) + 1;                    // by the last row of the tile
+  const int share = u.share ? u.share : ((seen + splits - 1) / splits + 15) & ~15;
+  const int s0 = (int)min((long long)u.split * share, (long long)seen), s1 = min(seen, s0 + share);
 
   MfmaTile<kChunkRows, ET> tile;
   const int my = min(lo, rows - 1), my_tok = token_of(my);
   const int my_end = min(s1, pos0 + my_tok + 1);                     // of query row lo
   {
-    const ET* p = q + (long long)(sc.row + my_tok) * q_stride + (long long)(h * G + (qt * kChunkRows + my) - my_tok * G) * D;
+    const ET* p = q + (long long)(u.seq.row + my_tok) * q_stride + (long long)(h * G + (qrow + my) - my_tok * G) * D;
 #pragma unroll
     for (int i = 0; i < (F32 ? 8 : 4); ++i)
       tile.qb[i] = __builtin_bit_cast(typename MfmaTile<kChunkRows, ET>::QT, *reinterpret_cast<const uint4*>(p + chunk_dim<ET, F>(i, hi)));
   }
   tile.reset();
 
-  const RT* Kh = K + h * cv.sh + (F == kPlain ? kChunk<ET> : 16) * hi;
-  const RT* Vh = V + h * cv.sh + 8 * lo;
-  const float* ksh = F == kPlain ? nullptr : cv.ks + h * cv.ssh;
-  const float* vsh = F == kPlain ? nullptr : cv.vs + h * cv.ssh;
+  const bool paged = cv.pm.table != nullptr;
+  const long long seq = (paged ? 0 : b * cv.sb) + h * cv.sh, sseq = (paged ? 0 : b * cv.ssb) + h * cv.ssh;
+  const RT* Kh = K + seq + (F == kPlain ? kChunk<ET> : 16) * hi;
+  const RT* Vh = V + seq + 8 * lo;
+  const float* ksh = F == kPlain ? nullptr : cv.ks + sseq;
+  const float* vsh = F == kPlain ? nullptr : cv.vs + sseq;
+  const long long sb = paged ? cv.sb : 0, ssb = paged ? cv.ssb : 0;
+  const int32_t* const table = paged ? cv.pm.table + (size_t)b * cv.pm.max_blocks : reinterpret_cast<const int32_t*>(q);   // (an entry is read in any case)
+  const int shift = paged ? cv.pm.shift : 31, in_block = paged ? (1 << cv.pm.shift) - 1 : 0x7fffffff, blk_max = paged ? cv.pm.n_pool - 1 : 0;
+  const auto block_of = [&](int n) FASA_INLINE { return min(max(table[n >> shift], 0), blk_max); };
   typename std::conditional<F == kPlain, TileKV<ET>, RawKV<ET, F>>::type raw;
   f32x4_t ks = {1.f, 1.f, 1.f, 1.f}, vs = ks;
-  struct Place { long long k, v[4], vs[4]; } pl;       // rows and scales of the next tile
-  // the tile's rows from token j0 on; tokens behind the split's last are the last again
-  auto find_rows = [&](int j0) FASA_INLINE {
+  struct Place { long long k, v[4], vs[4]; } pl;                     // rows and scales of the next tile
+  // Lane l: the block of this wave's l-th tile from here on.  A lookup between a tile's loads and the next one's would wait for the former.
+  int entries = 0;
+  auto look_up = [&](int j0) FASA_INLINE {
+    if constexpr (!SMALL) entries = block_of((int)min((long long)j0 + (long long)ROUND * lane, (long long)s1 - 1));
+  };
+  // rows from token j0 on, this wave's i-th tile since the lookup; tokens behind the split's last are the last again
+  auto find_rows = [&](int j0, int i) FASA_INLINE {
     if constexpr (SMALL) {
-      int blk, off;
-      cache_place(cv.pm, b, min(j0 + lo, s1 - 1), blk, off);
-      pl.k = blk * cv.sb + off * cv.sn;
+      const int nk = min(j0 + lo, s1 - 1);
+      pl.k = block_of(nk) * sb + (nk & in_block) * cv.sn;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        cache_place(cv.pm, b, min(j0 + 4 * hi + e, s1 - 1), blk, off);
-        pl.v[e] = blk * cv.sb + off * cv.sn;
-        pl.vs[e] = blk * cv.ssb + off;
+        const int n = min(j0 + 4 * hi + e, s1 - 1), blk = block_of(n);
+        pl.v[e] = blk * sb + (n & in_block) * cv.sn;
+        pl.vs[e] = blk * ssb + (n & in_block);
       }
     } else {
-      int blk, off;
-      cache_place(cv.pm, b, min(j0, (s1 - 1) & ~15), blk, off);      // (j0 is a multiple of 16, the same for the wave)
-      const int last = s1 - 1 - min(j0, (s1 - 1) & ~15);
-      const long long base = blk * cv.sb + off * cv.sn, sbase = blk * cv.ssb + off;
-      pl.k = base + (long long)min(lo, last) * cv.sn;
+      const int last = min(s1 - 1 - j0, 15), blk = __builtin_amdgcn_readlane(entries, i);     // (j0 is a multiple of 16)
+      const long long base = blk * sb + (j0 & in_block) * cv.sn;
+      pl.k = base + min(lo, last) * cv.sn;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pl.v[e] = base + (long long)min(4 * hi + e, last) * cv.sn;
-      pl.vs[0] = sbase + min(4 * hi, last & ~3);                     // four at once: rows of scales are whole fours
+      for (int e = 0; e < 4; ++e) pl.v[e] = base + min(4 * hi + e, last) * cv.sn;
+      pl.vs[0] = blk * ssb + (j0 & in_block) + min(4 * hi, last & ~3);                        // four at once: rows of scales are whole fours
     }
   };
-  auto load_k = [&]() FASA_INLINE {
-    raw.load_k(Kh + pl.k);
+  auto scales = [&](const float* from) FASA_INLINE {
+    f32x4_t x = {1.f, 1.f, 1.f, 1.f};
     if constexpr (F != kPlain) {
       if constexpr (SMALL) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ks[e] = ksh[pl.vs[e]];
+        for (int e = 0; e < 4; ++e) x[e] = from[pl.vs[e]];
       } else {
-        ks = *reinterpret_cast<const f32x4_t*>(ksh + pl.vs[0]);
+        x = *reinterpret_cast<const f32x4_t*>(from + pl.vs[0]);
       }
     }
+    return x;
   };
+  auto load_k = [&]() FASA_INLINE { raw.load_k(Kh + pl.k); ks = scales(ksh); };
   auto load_v = [&]() FASA_INLINE {
 #pragma unroll
     for (int e = 0; e < 4; ++e) raw.load_v(e, Vh + pl.v[e]);
-    if constexpr (F != kPlain) {
-      if constexpr (SMALL) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) vs[e] = vsh[pl.vs[e]];
-      } else {
-        vs = *reinterpret_cast<const f32x4_t*>(vsh + pl.vs[0]);
-      }
-    }
+    vs = scales(vsh);
   };
   int j0 = s0 + 16 * wave;
   if (j0 < s1) {
-    find_rows(j0);
+    look_up(j0);
+    find_rows(j0, 0);
     load_k();
     load_v();
-    TileKV<ET> kv;
-    for (; j0 < s1; j0 += kChunkStep) {
+    for (int i = 1; j0 < s1; j0 += ROUND, ++i) {
+      if ((i & 63) == 0) look_up(j0 + ROUND);
+      const bool more = j0 + ROUND < s1;
+      find_rows(more ? j0 + ROUND : j0, (more ? i : i - 1) & 63);     // (behind the last tile that tile again, for nobody)
       float sv[4];
-      f32x4_t k_by = ks, v_by = vs;
-      if constexpr (F == kPlain) kv = raw; else { raw.k_to(kv); raw.v_to(kv); }
-      find_rows(min(j0 + kChunkStep, s1 - 1) & ~15);                 // (behind the last tile: a tile that nobody takes)
-      load_k();
-      load_v();
-      tile.logits(kv, scale_log2e, sv);
+      auto seen_only = [&]() FASA_INLINE {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = j0 + 4 * hi + e;
-        // rows behind the split's end were not loaded, and the scales read there may be anything
-        if constexpr (F != kPlain) { sv[e] *= k_by[e]; v_by[e] = n < s1 ? v_by[e] : 0.f; }
-        sv[e] = n < my_end ? sv[e] : -INFINITY;
+        for (int e = 0; e < 4; ++e) sv[e] = j0 + 4 * hi + e < my_end ? sv[e] : -INFINITY;
+      };
+      if constexpr (F == kPlain) {
+        // One set of registers: the next tile's K goes where this one's has been used, and runs under this tile's P . V, its V under the next logits.
+        tile.logits(raw, scale_log2e, sv);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k();
+        __builtin_amdgcn_sched_barrier(0);
+        seen_only();
+        tile.accumulate_full(raw, sv, &scs[wave][0], lo, hi);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v();
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        // Values go into registers of their own, and all of the next tile is asked for at once.
+        TileKV<ET> kv;
+        const f32x4_t k_by = ks;
+        f32x4_t v_by;
+        // (scales behind the split's end were not this tile's and may be anything)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v_by[e] = j0 + 4 * hi + e < s1 ? vs[e] : 0.f;
+        raw.k_to(kv);
+        raw.v_to(kv);
+        load_k();
+        load_v();
+        tile.logits(kv, scale_log2e, sv);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sv[e] *= k_by[e];
+        seen_only();
+        tile.accumulate_full(kv, sv, &scs[wave][0], lo, hi, [&](int e, float w) FASA_INLINE { return w * v_by[e]; });
       }
-      if constexpr (F == kPlain) tile.accumulate_full(kv, sv, &scs[wave][0], lo, hi);
-      else tile.accumulate_full(kv, sv, &scs[wave][0], lo, hi, [&](int e, float w) { return w * v_by[e]; });
     }
   }
-  float* sm_m = lds + kChunkWaves * cap * D;
-  float* sm_l = sm_m + kChunkWaves * cap;
+  float* sm_m = lds + NWV * cap * D;
+  float* sm_l = sm_m + NWV * cap;
   tile.finish(sm_m + wave * cap, sm_l + wave * cap, lds + wave * cap * D, lo, hi, rows);
   __syncthreads();
 
   // row r of the tile, to O
   auto store_row = [&](int r, int d4, float4 a) FASA_INLINE {
     const int tok = token_of(r);
-    ET* o = O + (long long)(sc.row + tok) * o_stride + (long long)(h * G + (qt * kChunkRows + r) - tok * G) * D + 4 * d4;
+    ET* o = O + (long long)(u.seq.row + tok) * o_stride + (long long)(h * G + (qrow + r) - tok * G) * D + 4 * d4;
     if constexpr (F32) *reinterpret_cast<float4*>(o) = a;
     else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w));
   };
-  const size_t tile_id = (size_t)(b * Hkv + h) * tiles_each + qt;
-  float* pa = part_acc + tile_id * splits * cap * D;
-  float2* pm = reinterpret_cast<float2*>(part_ml) + tile_id * splits * cap;
-  for (int x = t; x < rows * (D / 4); x += kChunkThreads) {
+  // partial results: [head][unit][cap]
+  const size_t part0 = ((size_t)h * all_units + u.first) * cap;
+  float* pa = part_acc + part0 * D;
+  float2* pm = part_ml + part0;
+  for (int x = t; x < rows * (D / 4); x += NT) {
     const int r = x / (D / 4), d4 = x % (D / 4);
     float mn = kNegBig, l = 0.f;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < kChunkWaves; ++w) mn = fmaxf(mn, sm_m[w * cap + r]);
+    for (int w = 0; w < NWV; ++w) mn = fmaxf(mn, sm_m[w * cap + r]);
 #pragma unroll
-    for (int w = 0; w < kChunkWaves; ++w) {
+    for (int w = 0; w < NWV; ++w) {
       const float by = exp2f(sm_m[w * cap + r] - mn);
       l = fmaf(sm_l[w * cap + r], by, l);
       const float4 o = *reinterpret_cast<const float4*>(lds + (size_t)(w * cap + r) * D + 4 * d4);
@@ -210,15 +238,15 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
     if (splits == 1) {
       store_row(r, d4, make_float4(a.x / l, a.y / l, a.z / l, a.w / l));
     } else {
-      float2* to = reinterpret_cast<float2*>(pa + ((size_t)split * cap + r) * D + 4 * d4);
+      float2* to = reinterpret_cast<float2*>(pa + ((size_t)u.split * cap + r) * D + 4 * d4);
       st_agent(to, make_float2(a.x, a.y));
       st_agent(to + 1, make_float2(a.z, a.w));
-      if (d4 == 0) st_agent(pm + split * cap + r, make_float2(mn, l));
+      if (d4 == 0) st_agent(pm + (size_t)u.split * cap + r, make_float2(mn, l));
     }
   }
   if (splits == 1) return;
   publish_barrier();
-  uint32_t* tk = tickets + (size_t)(b * Hkv + h) * kChunkTickets + qt;
+  uint32_t* tk = tickets + (size_t)(b * Hkv + h) * kChunkTickets + kTicketWords * u.tile;
   if (t == 0) ticket = atomicAdd(tk, 1u);
   __syncthreads();
   if (ticket != (uint32_t)splits - 1u) return;
@@ -226,7 +254,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
 
   // ---- the tile's last workgroup merges ----
   float* w = lds;                                                     // [row][split]
-  for (int r = wave; r < rows; r += kChunkWaves) {
+  for (int r = wave; r < rows; r += NWV) {
     float mx = kNegBig, sum = 0.f;
     for (int sp = lane; sp < splits; sp += kWave) mx = fmaxf(mx, ld_agent(pm + sp * cap + r).x);
     mx = wave_max(mx);
@@ -241,18 +269,18 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
   }
   __syncthreads();
   const __amdgpu_buffer_rsrc_t rs = agent_buffer(pa);
-  for (int x = t; x < rows * (D / 4); x += kChunkThreads) {
+  for (int x = t; x < rows * (D / 4); x += NT) {
     const int r = x / (D / 4), d4 = x % (D / 4);
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int sp0 = 0; sp0 < splits; sp0 += 8) {
       uint4 o[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) o[u] = agent_load_u128(rs, (uint32_t)(((min(sp0 + u, splits - 1) * cap + r) * D + 4 * d4) * 4));
+      for (int k = 0; k < 8; ++k) o[k] = agent_load_u128(rs, (uint32_t)(((min(sp0 + k, splits - 1) * cap + r) * D + 4 * d4) * 4));
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float by = sp0 + u < splits ? w[r * splits + min(sp0 + u, splits - 1)] : 0.f;
-        a.x = fmaf(__uint_as_float(o[u].x), by, a.x); a.y = fmaf(__uint_as_float(o[u].y), by, a.y);
-        a.z = fmaf(__uint_as_float(o[u].z), by, a.z); a.w = fmaf(__uint_as_float(o[u].w), by, a.w);
+      for (int k = 0; k < 8; ++k) {
+        const float by = sp0 + k < splits ? w[r * splits + min(sp0 + k, splits - 1)] : 0.f;
+        a.x = fmaf(__uint_as_float(o[k].x), by, a.x); a.y = fmaf(__uint_as_float(o[k].y), by, a.y);
+        a.z = fmaf(__uint_as_float(o[k].z), by, a.z); a.w = fmaf(__uint_as_float(o[k].w), by, a.w);
       }
     }
     const float by = red[r];
@@ -260,24 +288,29 @@ __global__ __launch_bounds__(kChunkThreads, 2) void chunk_kernel(const ET* __res
   }
 }
 
-// Splits: as many as fill the compute units once, of 64 tokens or more, 256 at most (the merge's weights lie in LDS).
-ChunkPlan plan_chunk(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start) {
-  ChunkPlan p{};
+void plan_chunk_units(const fasa_shape& s, const ChunkView& ch, int rows, int resident, int resident_by_length, int least_share, int most_splits, ChunkPlan* p) {
   const int G = s.n_q_heads / s.n_kv_heads;
-  if (s.dtype == FASA_BF16 && (long long)n_new * G > kChunkRows) return plan_chunk_wide(s, apart, n_new, n_rows, by_row_start);
-  p.tile_rows = n_new * (long long)G < kChunkRows ? n_new * G : kChunkRows;
-  p.tiles = (int)chunk_tiles(by_row_start, s.batch, n_new, n_rows, G, kChunkRows);
-  p.per_seq = (int)(((long long)n_new * G + kChunkRows - 1) / kChunkRows);
-  const long long wgs = (long long)p.tiles * s.n_kv_heads;
-  long long n = kAssumedCUs / wgs;
-  const int most = (s.n_ctx + 63) / 64;
-  if (n > most) n = most;
-  if (n > 256) n = 256;
-  if (p.per_seq > kChunkTickets) n = 1;
-  p.splits = n < 1 ? 1 : (int)n;
-  const size_t parts = p.splits == 1 ? 0 : (size_t)s.batch * s.n_kv_heads * p.per_seq * p.splits * p.tile_rows;
-  p.part_acc_bytes = parts * kHeadDim * 4;
-  p.part_ml_bytes = parts * 8;
+  const long long tiles = chunk_tiles(ch.row_start != nullptr, s.batch, ch.n_new, ch.n_rows, G, rows);
+  const long long units = resident / s.n_kv_heads, units_by_length = resident_by_length / s.n_kv_heads;
+  p->tile_rows = rows;
+  p->per_seq = (int)(((long long)ch.n_new * G + rows - 1) / rows);
+  p->by_length = (ch.n_ctx_seq || ch.n_new_seq) && s.batch > 1 && s.batch <= kWave && tiles <= units_by_length;
+  const long long most = (s.n_ctx + least_share - 1) / least_share;
+  const long long n = std::min({units / tiles, most, (long long)most_splits});
+  p->splits = n < 1 ? 1 : (int)n;
+  p->units = (int)(p->by_length ? std::min(units_by_length, tiles * most) : tiles * p->splits);
+  const size_t parts = p->splits == 1 && !p->by_length ? 0 : (size_t)p->units * s.n_kv_heads * rows;
+  p->part_acc_bytes = parts * kHeadDim * 4;
+  p->part_ml_bytes = parts * 8;
+}
+
+// Tiles of 16 query rows, or of all that there are.
+ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch) {
+  const int G = s.n_q_heads / s.n_kv_heads;
+  if (s.dtype == FASA_BF16 && (long long)ch.n_new * G > kChunkRows) return plan_chunk_wide(s, apart, ch);
+  ChunkPlan p{};
+  const long long m = (long long)ch.n_new * G;
+  plan_chunk_units(s, ch, m < kChunkRows ? (int)m : kChunkRows, kChunkResident, 2 * kChunkResident, kChunkLeast, kChunkSplits, &p);
   return p;
 }
 
@@ -285,12 +318,12 @@ template <typename ET, CacheFmt F>
 static hipError_t chunk_t(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
   using RT = typename RowType<ET, F>::type;
   const bool small = a.cv.pm.table != nullptr && a.cv.pm.shift < 4;
-  const size_t totals = (size_t)kChunkWaves * p.tile_rows * (kHeadDim + 2) * 4, merge = (size_t)p.tile_rows * p.splits * 4;
+  const int hkv = s.n_kv_heads, G = s.n_q_heads / hkv;
+  const size_t totals = (size_t)kChunkWaves<ET, F> * p.tile_rows * (kHeadDim + 2) * 4, merge = (size_t)p.tile_rows * (p.by_length ? p.units : p.splits) * 4;
   const auto kernel = small ? chunk_kernel<ET, F, true> : chunk_kernel<ET, F, false>;
-  return launch_lds("fasa_chunk_attend", kernel, dim3((unsigned)((long long)p.tiles * s.n_kv_heads * p.splits)), dim3(kChunkThreads),
-                    totals > merge ? totals : merge, st, (const ET*)a.q, (const RT*)a.cv.K, (const RT*)a.cv.V, (ET*)a.O, a.part_acc, a.part_ml,
-                    a.tickets, a.cv, a.ch, s.batch, s.n_kv_heads, s.n_q_heads / s.n_kv_heads, p.per_seq, p.splits, p.tile_rows, a.q_stride,
-                    a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
+  return launch_lds("fasa_chunk_attend", kernel, dim3((unsigned)p.units * (unsigned)hkv), dim3(64 * kChunkWaves<ET, F>), totals > merge ? totals : merge, st,
+                    (const ET*)a.q, (const RT*)a.cv.K, (const RT*)a.cv.V, (ET*)a.O, a.part_acc, (float2*)a.part_ml, a.tickets, a.cv, a.ch, s.batch, hkv, G,
+                    p.per_seq, p.splits, p.by_length ? p.units : 0, p.units, p.tile_rows, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
 }
 
 hipError_t launch_chunk(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {

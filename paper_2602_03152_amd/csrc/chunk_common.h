@@ -79,6 +79,57 @@ __device__ __forceinline__ bool find_chunk_tile(const ChunkView& c, int batch, i
   }
   return false;
 }
+// A workgroup's part of the work: tokens [split * share, ..) of a query tile of a sequence.  first: the unit of the tile's split 0.
+struct ChunkUnit {
+  SeqChunk seq;
+  int b, tile, split, splits, first;
+  int share;                    // 0: the tile's tokens in equal parts
+};
+// Unit y of the grid.  Uniform: every tile in `splits` parts.  By length (units != 0; up to 64 sequences): a batch of mixed lengths would wait for its longest
+// sequence, so all parts are of about as many tokens, and a sequence has as many of them as it takes: the smallest share (a multiple of 64 tokens, of
+// least_share or more) with which all the tiles' parts are no more than the units.  Every wave finds it by itself, a lane a sequence.
+template <int TILE>
+__device__ __forceinline__ bool find_chunk_unit(const ChunkView& c, int batch, int G, int tiles_each, int splits, int units, int least_share, unsigned y, ChunkUnit& u) {
+  if (units == 0) {
+    u.split = (int)(y % (unsigned)splits);
+    u.splits = splits;
+    u.first = (int)y - u.split;
+    u.share = 0;
+    if (!find_chunk_tile<TILE>(c, batch, G, tiles_each, y / (unsigned)splits, u.b, u.tile)) return false;
+    u.seq = seq_chunk(c, u.b);
+    return u.tile < (int)(((long long)u.seq.n_new * G + TILE - 1) / TILE);
+  }
+  SeqChunk s = {0, 0, 0};
+  if (lane_id() < batch) s = seq_chunk(c, lane_id());
+  const int nt = (int)(((long long)s.n_new * G + TILE - 1) / TILE);
+  const int s64 = nt ? (int)(((long long)s.n_ctx + 63) / 64) : 0;
+  const auto parts = [&](int q) {                                      // of a tile, with a share of q times 64 tokens
+    int n = (int)ceilf((float)s64 * __builtin_amdgcn_rcpf((float)q));
+    if ((long long)n * q < s64) ++n;
+    return n;
+  };
+  int hi = max((int)wave_max((float)s64) + 1, 1);                      // (holds all; + 1 for what the conversion may round off)
+  int lo = min(max((int)(wave_sum((float)nt * (float)s64) / (float)units), least_share / 64), hi);
+  for (int i = 0; i < 8 && lo < hi; ++i) {
+    const int mid = (lo + hi) / 2;
+    if (wave_sum((float)nt * (float)parts(mid)) <= (float)units) hi = mid;
+    else lo = mid + 1;
+  }
+  const int n = parts(hi);
+  const uint32_t v = (uint32_t)(nt * n), incl = wave_prefix_sum(v);
+  const unsigned long long reached = __ballot(incl > y);
+  // (more parts than units: only if the sequences' rows overlap, so that there are more new tokens than rows)
+  if (reached == 0ull || __builtin_amdgcn_readlane((int)incl, kWave - 1) > units) return false;
+  u.b = __builtin_ctzll(reached);
+  const int local = (int)y - __builtin_amdgcn_readlane((int)(incl - v), u.b);
+  u.splits = __builtin_amdgcn_readlane(n, u.b);
+  u.tile = local / u.splits;
+  u.split = local - u.tile * u.splits;
+  u.first = (int)y - u.split;
+  u.share = 64 * hi;
+  u.seq = SeqChunk{__builtin_amdgcn_readlane(s.n_ctx, u.b), __builtin_amdgcn_readlane(s.n_new, u.b), __builtin_amdgcn_readlane(s.row, u.b)};
+  return true;
+}
 // tiles that the grid needs (an upper bound)
 inline long long chunk_tiles(bool by_row_start, int batch, int n_new, int n_rows, int per_row, int tile) {
   return by_row_start ? (long long)n_rows * per_row / tile + batch : (long long)batch * (((long long)n_new * per_row + tile - 1) / tile);
@@ -116,20 +167,25 @@ hipError_t launch_cache_write(const fasa_shape& s, const CacheView& cv, CacheFmt
 hipError_t launch_cache_read(const fasa_shape& s, const CacheView& cv, CacheFmt fmt, const int32_t* T, const int32_t* n_ctx_seq,
                              int n_begin, int n_end, void* K_out, void* V_out, hipStream_t st);
 
-// How a chunk is attended.  wide: by chunk_wide.hip.  tiles: of the grid; per_seq: query tiles of the longest sequence; splits: of a tile's tokens.
+// How a chunk is attended.  wide: by chunk_wide.hip.
 struct ChunkPlan {
   bool wide;
   bool apart;         // wide: rows are looked up one by one
+  bool by_length;     // parts by the sequences' lengths
   int tile_rows;      // query rows (new token, head of the group) of a tile
-  int tiles, per_seq, splits;
+  int per_seq;        // query tiles of the longest sequence
+  int splits;         // parts of a tile, where it is not by_length
+  int units;          // workgroups of a KV head, at most
   size_t part_acc_bytes, part_ml_bytes;
 };
+// units, splits and partial results, for tiles of `rows` query rows: as many workgroups as are to be resident at once, of least_share tokens or more.
+void plan_chunk_units(const fasa_shape& s, const ChunkView& ch, int rows, int resident, int resident_by_length, int least_share, int most_splits, ChunkPlan* p);
 // apart: chunk_wide.hip has to look rows up one by one - pages of fewer tokens than a wave's load has rows, or strides beyond what it multiplies in 32 bits
 inline bool chunk_rows_apart(const CacheView& cv, CacheFmt fmt) {
   return (cv.pm.table != nullptr && ((1 << cv.pm.shift) < (fmt == kPlain ? 4 : 8) || cv.sb >= (1ll << 31))) || cv.sn >= (1ll << 27);
 }
-ChunkPlan plan_chunk(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start);
-ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start);
+ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch);
+ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, const ChunkView& ch);
 struct ChunkArgs {
   CacheView cv;
   ChunkView ch;

@@ -29,30 +29,30 @@ __device__ __forceinline__ uint2 lds_read_tr(lds_ptr p) {
   return __builtin_bit_cast(uint2, r);
 }
 
-// What a workgroup works on: query rows [qt TR, qt TR + rows) of sequence b and KV head h, tokens [s0, s1).
+// What a workgroup works on: query rows [qt TR, qt TR + rows) of sequence b and KV head h, tokens [s0, s1).  part: where its partial result goes.
+constexpr int kWideLeast = 256;                           // tokens of a part, at least
 template <int TR> struct WideJob {
-  int b, h, qt, split, rows, row0, pos0, s0, s1, n_tiles;
+  int b, h, qt, splits, rows, row0, pos0, s0, s1, n_tiles;
+  size_t part;
   __device__ __forceinline__ int token_of(int r, int G) const { return (qt * TR + r) / G; }      // new token of the tile's row r
-  // False: nothing to do.  Workgroups: heads fastest (those of a sequence read the same blocks, and a head's lie on one XCD where there are eight), then splits.
-  __device__ __forceinline__ bool find(const ChunkView& ch, int batch, int Hkv, int G, int tiles_each, int splits) {
-    unsigned id = blockIdx.x;
-    h = (int)(id % (unsigned)Hkv);
-    id /= (unsigned)Hkv;
-    split = (int)(id % (unsigned)splits);
-    id /= (unsigned)splits;
-    if (!find_chunk_tile<TR>(ch, batch, G, tiles_each, id, b, qt)) return false;
-    const SeqChunk sc = seq_chunk(ch, b);
-    const int m = sc.n_new * G, m_tiles = (m + TR - 1) / TR;
-    if (qt >= m_tiles) return false;
-    qt = m_tiles - 1 - qt;                                 // the longest first
+  // False: nothing to do.  Workgroups: heads fastest (those of a sequence read the same blocks, and a head's lie on one XCD where there are eight).
+  __device__ __forceinline__ bool find(const ChunkView& ch, int batch, int Hkv, int G, int tiles_each, int all_splits, int units, int all_units) {
+    h = (int)(blockIdx.x % (unsigned)Hkv);
+    ChunkUnit u;
+    if (!find_chunk_unit<TR>(ch, batch, G, tiles_each, all_splits, units, kWideLeast, blockIdx.x / (unsigned)Hkv, u)) return false;
+    b = u.b;
+    splits = u.splits;
+    const int m = u.seq.n_new * G;
+    qt = (m + TR - 1) / TR - 1 - u.tile;                   // the longest first
     rows = min(TR, m - qt * TR);
-    row0 = sc.row;
-    pos0 = sc.n_ctx - sc.n_new;
+    row0 = u.seq.row;
+    pos0 = u.seq.n_ctx - u.seq.n_new;
     const int seen = pos0 + token_of(rows - 1, G) + 1;     // tokens that the tile's last row sees
-    const int share = ((seen + splits - 1) / splits + kWideTok - 1) / kWideTok * kWideTok;
-    s0 = min(split * share, seen);
+    const int share = u.share ? u.share : ((seen + splits - 1) / splits + kWideTok - 1) / kWideTok * kWideTok;
+    s0 = (int)min((long long)u.split * share, (long long)seen);
     s1 = min(seen, s0 + share);
     n_tiles = (s1 - s0 + kWideTok - 1) / kWideTok;
+    part = (size_t)h * all_units + u.first + u.split;
     return true;
   }
 };
@@ -262,11 +262,11 @@ template <bool BYTES> struct WideQueries {
   }
   // To O, or where there are splits to their places.  row: of the tile, before it was clamped.
   template <int TR>
-  __device__ __forceinline__ void finish(const WideJob<TR>& job, int row, uint16_t* O, long long o_stride, int G, float* part_acc, float2* part_ml, int Hkv, int tiles_each, int splits) {
+  __device__ __forceinline__ void finish(const WideJob<TR>& job, int row, uint16_t* O, long long o_stride, int G, float* part_acc, float2* part_ml) {
     constexpr int D = kHeadDim;
     const float l = xor32_sum(l_run);
     if (row >= job.rows) return;
-    if (splits == 1) {
+    if (job.splits == 1) {
       const float by = 1.0f / l;
       const int tok = job.token_of(my, G);
       uint16_t* o = O + (long long)(job.row0 + tok) * o_stride + (long long)(job.h * G + (job.qt * TR + my) - tok * G) * D + 4 * half;
@@ -277,7 +277,7 @@ template <bool BYTES> struct WideQueries {
           *reinterpret_cast<uint2*>(o + 32 * d + 8 * g) = make_uint2(pack_bf16(oc[d][4 * g] * by, oc[d][4 * g + 1] * by), pack_bf16(oc[d][4 * g + 2] * by, oc[d][4 * g + 3] * by));
       return;
     }
-    const size_t to = (((size_t)(job.b * Hkv + job.h) * tiles_each + job.qt) * splits + job.split) * TR + my;
+    const size_t to = job.part * TR + my;
     float* pa = part_acc + to * D + 4 * half;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -294,13 +294,13 @@ template <CacheFmt F, bool APART>
 __global__ __launch_bounds__(64 * kShortWaves, 2) void chunk_short_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
                                                                          uint16_t* __restrict__ O, float* __restrict__ part_acc,
                                                                          float2* __restrict__ part_ml, CacheView cv, ChunkView ch, int batch, int Hkv,
-                                                                         int G, int tiles_each, int splits, long long q_stride, long long o_stride,
+                                                                         int G, int tiles_each, int splits, int units, int all_units, long long q_stride, long long o_stride,
                                                                          float scale_log2e) {
   constexpr bool BYTES = F != kPlain;
   extern __shared__ __align__(16) unsigned char smem[];    // [2][K tile, V tile], then scales [2][k 64, v 64]
   float* const sm_scale = reinterpret_cast<float*>(smem + 4 * kTileBytes);
   WideJob<kShortRows> job;
-  if (!job.find(ch, batch, Hkv, G, tiles_each, splits)) return;
+  if (!job.find(ch, batch, Hkv, G, tiles_each, splits, units, all_units)) return;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   using Loader = WideLoader<F, kShortWaves, APART>;
   const Loader ld(cv, K, V, q, job.b, job.h, job.s1, wave, lane);
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void chunk_short_kernel(const 
       __syncthreads();
     }
   }
-  wq.finish(job, 32 * wave + (lane & 31), O, o_stride, G, part_acc, part_ml, Hkv, tiles_each, splits);
+  wq.finish(job, 32 * wave + (lane & 31), O, o_stride, G, part_acc, part_ml);
 }
 
 // Many: eight waves (256 rows a tile), two a SIMD.  In steps of 32 tokens: step u runs the logits of step u + 1 and the output of step u - 1 ahead of its own
@@ -363,7 +363,7 @@ template <CacheFmt F>
 __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
                                                                        uint16_t* __restrict__ O, float* __restrict__ part_acc,
                                                                        float2* __restrict__ part_ml, CacheView cv, ChunkView ch, int batch, int Hkv,
-                                                                       int G, int tiles_each, int splits, long long q_stride, long long o_stride,
+                                                                       int G, int tiles_each, int splits, int units, int all_units, long long q_stride, long long o_stride,
                                                                        float scale_log2e) {
   constexpr int NT = 64 * kDeepWaves, B = kTileBytes;
   constexpr bool BYTES = F != kPlain;
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
   float* const ssk = reinterpret_cast<float*>(smem + 2 * kDeepSlots * B);
   float* const ssv = ssk + kDeepSlots * kWideTok;
   WideJob<kDeepRows> job;
-  if (!job.find(ch, batch, Hkv, G, tiles_each, splits)) return;
+  if (!job.find(ch, batch, Hkv, G, tiles_each, splits, units, all_units)) return;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   using Loader = WideLoader<F, kDeepWaves, false>;
   using Rows = typename Loader::Rows;
@@ -436,47 +436,66 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
     }
     wq.output((lds_ptr)smv + c2 * B + 32 * 256, pa);
   }
-  wq.finish(job, 32 * wave + (lane & 31), O, o_stride, G, part_acc, part_ml, Hkv, tiles_each, splits);
+  wq.finish(job, 32 * wave + (lane & 31), O, o_stride, G, part_acc, part_ml);
 }
 
-// Joins the splits of a tile's rows: 32 lanes a row, four dims each.
+// Joins the parts of a tile's rows: as many workgroups for each part, which take as many rows as the others, 32 lanes a row, four dims each.
+template <int TR> constexpr int kMergeWgs = TR / 64;
 template <int TR>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restrict__ part_acc, const float2* __restrict__ part_ml, uint16_t* __restrict__ O,
-                                                          ChunkView ch, int batch, int Hkv, int G, int tiles_each, int splits, long long o_stride) {
-  const int h = blockIdx.y;
-  unsigned id = blockIdx.x / (TR / 8);
-  const int r = (int)(blockIdx.x % (TR / 8)) * 8 + (int)(threadIdx.x >> 5), c = threadIdx.x & 31;
-  int b, qt;
-  if (!find_chunk_tile<TR>(ch, batch, G, tiles_each, id, b, qt)) return;
-  const SeqChunk sc = seq_chunk(ch, b);
-  if (qt * (long long)TR + r >= (long long)sc.n_new * G) return;
-  const size_t at = ((size_t)(b * Hkv + h) * tiles_each + qt) * splits * TR + r;
-  float mx = kNegBig, l = 0.f;
-  for (int s = 0; s < splits; ++s) mx = fmaxf(mx, part_ml[at + (size_t)s * TR].x);
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    const float2 ml = part_ml[at + (size_t)s * TR];
-    const float by = exp2f(ml.x - mx);
-    const float4 x = *reinterpret_cast<const float4*>(part_acc + (at + (size_t)s * TR) * kHeadDim + 4 * c);
-    l = fmaf(ml.y, by, l);
-    a.x = fmaf(x.x, by, a.x); a.y = fmaf(x.y, by, a.y); a.z = fmaf(x.z, by, a.z); a.w = fmaf(x.w, by, a.w);
+                                                          ChunkView ch, int batch, int Hkv, int G, int tiles_each, int all_splits, int units, int all_units,
+                                                          long long o_stride) {
+  extern __shared__ float weights[];                                   // [8][parts]
+  const int h = (int)(blockIdx.x % (unsigned)Hkv);
+  ChunkUnit u;
+  if (!find_chunk_unit<TR>(ch, batch, G, tiles_each, all_splits, units, kWideLeast, blockIdx.x / (unsigned)Hkv, u) || u.splits == 1) return;
+  const int wgs = u.splits * kMergeWgs<TR>, wg = u.split * kMergeWgs<TR> + (int)blockIdx.y;
+  const int n = u.splits, m = u.seq.n_new * G, qt = (m + TR - 1) / TR - 1 - u.tile, rows = min(TR, m - qt * TR);
+  const int group = threadIdx.x >> 5, c = threadIdx.x & 31;
+  const size_t part0 = ((size_t)h * all_units + u.first) * TR;
+  float* const w = weights + group * n;
+  const int per = (rows + wgs - 1) / wgs, r1 = min(rows, (wg + 1) * per);
+  for (int r = wg * per + group; r < r1; r += 8) {
+    const float2* ml = part_ml + part0 + r;
+    float mx = kNegBig, l = 0.f;
+    for (int s = c; s < n; s += 32) mx = fmaxf(mx, ml[(size_t)s * TR].x);
+    mx = xor16_max(row16_max(mx));                                     // (of 32 lanes)
+    for (int s = c; s < n; s += 32) {
+      const float2 x = ml[(size_t)s * TR];
+      w[s] = exp2f(x.x - mx);
+      l = fmaf(x.y, w[s], l);
+    }
+    l = xor16_sum(row16_sum(l));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // (a wave's LDS operations complete in order)
+    const float* pa = part_acc + (part0 + r) * kHeadDim + 4 * c;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < n; s0 += 8) {
+      float4 x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = *reinterpret_cast<const float4*>(pa + (size_t)min(s0 + k, n - 1) * TR * kHeadDim);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float by = s0 + k < n ? w[min(s0 + k, n - 1)] : 0.f;
+        a.x = fmaf(x[k].x, by, a.x); a.y = fmaf(x[k].y, by, a.y); a.z = fmaf(x[k].z, by, a.z); a.w = fmaf(x[k].w, by, a.w);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int row = qt * TR + r, tok = row / G;
+    const float by = 1.0f / l;
+    *reinterpret_cast<uint2*>(O + (long long)(u.seq.row + tok) * o_stride + (long long)(h * G + row - tok * G) * kHeadDim + 4 * c) =
+        make_uint2(pack_bf16(a.x * by, a.y * by), pack_bf16(a.z * by, a.w * by));
   }
-  const int row = qt * TR + r, tok = row / G;
-  const float by = 1.0f / l;
-  *reinterpret_cast<uint2*>(O + (long long)(sc.row + tok) * o_stride + (long long)(h * G + row - tok * G) * kHeadDim + 4 * c) =
-      make_uint2(pack_bf16(a.x * by, a.y * by), pack_bf16(a.z * by, a.w * by));
 }
 
 template <int TR, class Kernel>
 static hipError_t wide_t(Kernel kernel, size_t lds, const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
-  const int hkv = s.n_kv_heads, G = s.n_q_heads / hkv;
-  const hipError_t e = launch_lds("fasa_chunk_attend", kernel, dim3((unsigned)((long long)p.tiles * hkv * p.splits)), dim3(2 * TR), lds, st, (const uint16_t*)a.q,
+  const int hkv = s.n_kv_heads, G = s.n_q_heads / hkv, units = p.by_length ? p.units : 0;
+  const hipError_t e = launch_lds("fasa_chunk_attend", kernel, dim3((unsigned)p.units * (unsigned)hkv), dim3(2 * TR), lds, st, (const uint16_t*)a.q,
                                   (const void*)a.cv.K, (const void*)a.cv.V, (uint16_t*)a.O, a.part_acc, (float2*)a.part_ml, a.cv, a.ch, s.batch, hkv, G,
-                                  p.per_seq, p.splits, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
-  if (e != hipSuccess || p.splits == 1) return e;
-  return launch("fasa_chunk_merge", chunk_merge_kernel<TR>, dim3((unsigned)p.tiles * (TR / 8), hkv), dim3(256), st, (const float*)a.part_acc,
-                (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.splits, a.o_stride);
+                                  p.per_seq, p.splits, units, p.units, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
+  if (e != hipSuccess || (p.splits == 1 && !p.by_length)) return e;
+  return launch_lds("fasa_chunk_merge", chunk_merge_kernel<TR>, dim3((unsigned)p.units * (unsigned)hkv, kMergeWgs<TR>), dim3(256), (p.by_length ? p.units : p.splits) * 8 * sizeof(float),
+                    st, (const float*)a.part_acc, (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.splits, units, p.units, a.o_stride);
 }
 template <CacheFmt F> static hipError_t wide_f(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
   const size_t scales = F == kPlain ? 0 : kWideTok * 4;
@@ -487,25 +506,13 @@ hipError_t launch_chunk_wide(const fasa_shape& s, const ChunkPlan& p, const Chun
   return a.fmt == kPlain ? wide_f<kPlain>(s, p, a, st) : a.fmt == kInt8 ? wide_f<kInt8>(s, p, a, st) : wide_f<kE4m3>(s, p, a, st);
 }
 
-// Rows of 256, of 128 where a KV head has no more or where rows have to be looked up one by one.  Splits: as many as fill the compute units once (128: two
-// workgroups a compute unit), of 256 tokens or more.
-ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, int n_new, int n_rows, bool by_row_start) {
+// Tiles of 256 rows, of 128 where a KV head has no more or where rows have to be looked up one by one: two workgroups a compute unit then.
+ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, const ChunkView& ch) {
   ChunkPlan p{};
-  const int G = s.n_q_heads / s.n_kv_heads;
-  const long long m = (long long)n_new * G;
   p.wide = true;
   p.apart = apart;
-  p.tile_rows = m <= kShortRows || apart ? kShortRows : kDeepRows;
-  p.tiles = (int)chunk_tiles(by_row_start, s.batch, n_new, n_rows, G, p.tile_rows);
-  p.per_seq = (int)((m + p.tile_rows - 1) / p.tile_rows);
-  long long n = kAssumedCUs * (p.tile_rows == kShortRows ? 2 : 1) / ((long long)p.tiles * s.n_kv_heads);
-  const int most = (s.n_ctx + 255) / 256;
-  if (n > most) n = most;
-  if (n > 64) n = 64;
-  p.splits = n < 1 ? 1 : (int)n;
-  const size_t parts = p.splits == 1 ? 0 : (size_t)s.batch * s.n_kv_heads * p.per_seq * p.splits * p.tile_rows;
-  p.part_acc_bytes = parts * kHeadDim * 4;
-  p.part_ml_bytes = parts * 8;
+  const bool few = (long long)ch.n_new * (s.n_q_heads / s.n_kv_heads) <= kShortRows || apart;
+  plan_chunk_units(s, ch, few ? kShortRows : kDeepRows, few ? 2 * kAssumedCUs : kAssumedCUs, few ? 2 * kAssumedCUs : kAssumedCUs, kWideLeast, 64, &p);
   return p;
 }
 
