@@ -1,11 +1,11 @@
 // Rows of new tokens into the cache, in its format, and rows of the cache back in dtype.  Both move memory and little else:
-// a row is 16 lanes' work, eight values (16 bytes of bf16) a lane, and every lane has several rows in flight.
+// a row is 16 lanes' work, eight values (16 bytes of bf16) a lane, one row of K and one of V each.  (More rows a lane in flight, and fewer waves, are slower: 1 / 2 / 4 / 8
+// rows, 32768 x 8 written as e4m3 46 / 48 / 54 / 62 us, read from int8 41 / 41 / 43.5 / 48.)
 #include "chunk_common.h"
 
 namespace fasa {
 
-constexpr int kRowsInFlight = 4;                       // of K, and as many of V, per 16 lanes
-constexpr int kCacheTile = 16 * kRowsInFlight;         // (row, head) items of a workgroup of 256
+constexpr int kCacheTile = 16;                         // rows of K, and of V, of a workgroup of 256
 
 // largest of the 16 lanes of a row
 __device__ __forceinline__ uint32_t row16_max_u32(uint32_t x) {
@@ -46,19 +46,13 @@ template <CacheFmt F> __device__ __forceinline__ uint32_t codes_of(const float* 
     return __builtin_amdgcn_perm(cd, ab, 0x05040100u);
   }
 }
-// The quotient x / s as a float32 that rounds to any shorter format as the quotient itself does: cut, with the last bit set if anything was cut off
-// (two floats of 24 bits: a quotient that is no tie of a format of 8 bits differs from one by 2^-34 of it, which float64 holds).
-__device__ __forceinline__ float quotient_to_odd(float x, float s) {
-  const double y = (double)x / (double)s;
-  float f = (float)y;
-  const double back = (double)f;
-  if (back != y && (__float_as_uint(f) & 1u) == 0u) f = __uint_as_float(__float_as_uint(f) + (fabs(back) < fabs(y) ? 1u : ~0u));
-  return f;
-}
+// The values that four codes stand for.
+template <CacheFmt F> __device__ __forceinline__ f32x4_t values_of(uint32_t w) { return bytes_to_f32<F>(w); }
 
-// A row's eight values of this lane -> codes, and the row's scale.  codes: the nearest to x / s, decided as if the quotient were exact
-// - a product with 1 / s is off by up to 2^-23 of itself, which matters only within that of a tie: where the codes of 2^-21 less
-// and 2^-21 more differ (one lane in some 10^4), the wave divides in float64.  Dividing every value in float32 takes ten instructions more a value.
+// A row's eight values of this lane -> codes, and the row's scale.  codes: the nearest to x / s, decided as if the quotient were exact.  A product with 1 / s is off
+// by less than 2^-22 of itself, which matters only within that of a tie: where the codes of 2^-21 less and 2^-21 more differ (a lane in 10^3 for int8, in 10^4 for e4m3) the
+// nearest is one of the two, and x is compared with the middle between them times s: the difference is rounded once and has its exact sign.  (Dividing every value
+// takes ten instructions more each.)
 template <typename ET, CacheFmt F> __device__ __forceinline__ uint2 quantise_row(const Vals8<ET>& v, float& scale) {
   constexpr float Q = F == kE4m3 ? 448.f : 127.f;
   float f[8];
@@ -68,9 +62,16 @@ template <typename ET, CacheFmt F> __device__ __forceinline__ uint2 quantise_row
   for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);
   most = row16_max_u32(most);
   const bool finite = most < 0x7f800000u;
-  const float s = __uint_as_float(most) / Q;
+  float s = __uint_as_float(most) / Q;
   scale = finite ? s : __uint_as_float(0x7fc00000u);
-  const float inv = 1.0f / s;
+  const bool some = finite && s > 0.f, tiny = s < 0x1p-60f;
+  if (__ballot(some && tiny) != 0ull) {                    // (1 / s would be infinite, and differences below what float32 holds)
+    const float up = tiny ? 0x1p80f : 1.f;
+    s *= up;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= up;
+  }
+  const float inv = __builtin_amdgcn_rcpf(s);              // (within 2^-23)
   float lo[8], hi[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -80,18 +81,33 @@ template <typename ET, CacheFmt F> __device__ __forceinline__ uint2 quantise_row
   }
   uint2 c = make_uint2(codes_of<F>(lo), codes_of<F>(lo + 4));
   const uint2 d = make_uint2(codes_of<F>(hi), codes_of<F>(hi + 4));
-  const bool near = c.x != d.x || c.y != d.y || !(s >= 0x1p-120f);       // (below that 1 / s may be infinite)
-  if (__ballot(near && finite && most != 0u) != 0ull) {
+  const bool near = some && (c.x != d.x || c.y != d.y || tiny);
+  if (__ballot(near) != 0ull) {
     if (near) {
+      if (tiny) {                                          // (a scale of a few bits may leave quotients beyond Q)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) lo[i] = fminf(fmaxf(quotient_to_odd(f[i], s), -Q), Q);
+        for (int i = 0; i < 8; ++i) { lo[i] = fminf(fmaxf(lo[i], -Q), Q); hi[i] = fminf(fmaxf(hi[i], -Q), Q); }
+        c = make_uint2(codes_of<F>(lo), codes_of<F>(lo + 4));
+      }
+      const uint2 e = make_uint2(codes_of<F>(hi), codes_of<F>(hi + 4));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4_t vl = values_of<F>(h ? c.y : c.x), vh = values_of<F>(h ? e.y : e.x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float mid = 0.5f * (vl[i] + vh[i]), over = fmaf(-mid, s, f[4 * h + i]);
+          // (a tie: the middle itself, which goes to the even code)
+          lo[4 * h + i] = over > 0.f ? fmaxf(vl[i], vh[i]) : over < 0.f ? fminf(vl[i], vh[i]) : mid;
+        }
+      }
       c = make_uint2(codes_of<F>(lo), codes_of<F>(lo + 4));
     }
   }
-  return finite && s > 0.f ? c : make_uint2(0u, 0u);
+  return some ? c : make_uint2(0u, 0u);
 }
 
-// grid: tiles of kCacheTile (row, head) items of a sequence
+// grid: tiles of 16 (token, head) items of a sequence, as they lie in k_new.  (16 tokens of a head, whose scales are then written 64 bytes at a time, are 1 us faster
+// at 46, and 1 us slower for rows of dtype.)
 template <typename ET, CacheFmt F>
 __global__ __launch_bounds__(256) void cache_write_kernel(const ET* __restrict__ k_new, const ET* __restrict__ v_new, CacheView cv, ChunkView ch,
                                                           int batch, int Hkv, uint32_t m_hkv, int tiles_each, long long kv_stride) {
@@ -101,42 +117,34 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const ET* __restrict__
   const SeqChunk sc = seq_chunk(ch, b);
   const int n_items = sc.n_new * Hkv;
   const int group = threadIdx.x >> 4, c = threadIdx.x & 15;
-  const int j0 = tile * kCacheTile + group;
   if (tile * kCacheTile >= n_items) return;
-  Vals8<ET> k[kRowsInFlight], v[kRowsInFlight];
-  int head[kRowsInFlight], blk[kRowsInFlight], off[kRowsInFlight];
+  // (items behind the last are the last again: their lanes compute and do not store)
+  const int item = min(tile * kCacheTile + group, n_items - 1);
+  const int i = (int)fast_div((uint32_t)item, (uint32_t)Hkv, m_hkv), h = item - i * Hkv;
+  const long long from = (long long)(sc.row + i) * kv_stride + h * kHeadDim + 8 * c;
+  const Vals8<ET> k = load_vals<ET>(k_new + from), v = load_vals<ET>(v_new + from);
+  int blk, off;
+  cache_place(cv.pm, b, sc.n_ctx - sc.n_new + i, blk, off);
+  const bool mine = tile * kCacheTile + group < n_items;
+  const long long at = blk * cv.sb + h * cv.sh + off * cv.sn + 8 * c;
+  if constexpr (F == kPlain) {
+    if (mine) {
 #pragma unroll
-  for (int u = 0; u < kRowsInFlight; ++u) {
-    // (items behind the last are the last again: its lanes compute and do not store)
-    const int j = min(j0 + 16 * u, n_items - 1);
-    const int i = (int)fast_div((uint32_t)j, (uint32_t)Hkv, m_hkv);
-    head[u] = j - i * Hkv;
-    const long long at = (long long)(sc.row + i) * kv_stride + head[u] * kHeadDim + 8 * c;
-    k[u] = load_vals<ET>(k_new + at);
-    v[u] = load_vals<ET>(v_new + at);
-    cache_place(cv.pm, b, sc.n_ctx - sc.n_new + i, blk[u], off[u]);
-  }
-#pragma unroll
-  for (int u = 0; u < kRowsInFlight; ++u) {
-    const bool mine = j0 + 16 * u < n_items;
-    const long long at = blk[u] * cv.sb + head[u] * cv.sh + off[u] * cv.sn + 8 * c;
-    if constexpr (F == kPlain) {
-      if (mine) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(ET) / 2; ++i) {
-          reinterpret_cast<uint4*>((RT*)cv.K + at)[i] = k[u].w[i];
-          reinterpret_cast<uint4*>((RT*)cv.V + at)[i] = v[u].w[i];
-        }
+      for (int x = 0; x < (int)sizeof(ET) / 2; ++x) {
+        reinterpret_cast<uint4*>((RT*)cv.K + at)[x] = k.w[x];
+        reinterpret_cast<uint4*>((RT*)cv.V + at)[x] = v.w[x];
       }
-    } else {
-      float ks, vs;
-      const uint2 kc = quantise_row<ET, F>(k[u], ks), vc = quantise_row<ET, F>(v[u], vs);
-      if (mine) {
-        *reinterpret_cast<uint2*>((RT*)cv.K + at) = kc;
-        *reinterpret_cast<uint2*>((RT*)cv.V + at) = vc;
-        const long long sat = blk[u] * cv.ssb + head[u] * cv.ssh + off[u];
-        if (c == 0) cv.ks[sat] = ks;
-        if (c == 1) cv.vs[sat] = vs;
+    }
+  } else {
+    float ks, vs;
+    const uint2 kc = quantise_row<ET, F>(k, ks), vc = quantise_row<ET, F>(v, vs);
+    if (mine) {
+      *reinterpret_cast<uint2*>((RT*)cv.K + at) = kc;
+      *reinterpret_cast<uint2*>((RT*)cv.V + at) = vc;
+      const long long sat = blk * cv.ssb + h * cv.ssh + off;
+      if (c == 0) {
+        cv.ks[sat] = ks;
+        cv.vs[sat] = vs;
       }
     }
   }
@@ -164,51 +172,37 @@ template <typename ET, CacheFmt F> __device__ __forceinline__ void store_vals(ET
   }
 }
 
-// grid (tiles of kCacheTile tokens or list entries, rows)
+// grid (tiles of kCacheTile tokens or list entries, rows).  (Heads fastest: 42.0 / 40.8 us, 32768 x 8 int8; a selection 38.8 / 37.6.)
 template <typename ET, CacheFmt F>
 __global__ __launch_bounds__(256) void cache_read_kernel(ET* __restrict__ K_out, ET* __restrict__ V_out, CacheView cv, const int32_t* __restrict__ T,
-                                                         int t_pitch, int budget, const int32_t* __restrict__ n_ctx_seq, int n_ctx, int Hkv,
+                                                         int t_pitch, const int32_t* __restrict__ n_ctx_seq, int n_ctx, int Hkv,
                                                          uint32_t m_hkv, int n_begin, int n_end) {
   using RT = typename RowType<ET, F>::type;
   const int row = blockIdx.y;
   int b, h;
   head_of_row(row, Hkv, m_hkv, b, h);
   const int N = n_ctx_seq ? min(max(n_ctx_seq[b], 0), n_ctx) : n_ctx;
-  const int end = min(n_end, T ? min(budget, N) : N);
-  const int group = threadIdx.x >> 4, c = threadIdx.x & 15;
-  const int j0 = n_begin + blockIdx.x * kCacheTile + group;
-  if (n_begin + (int)blockIdx.x * kCacheTile >= end) return;
-  int blk[kRowsInFlight], off[kRowsInFlight];
-  float ks[kRowsInFlight], vs[kRowsInFlight];
-#pragma unroll
-  for (int u = 0; u < kRowsInFlight; ++u) {
-    const int j = min(j0 + 16 * u, end - 1);
-    const int n = T ? min(max(T[(size_t)row * t_pitch + j], 0), N - 1) : j;
-    cache_place(cv.pm, b, n, blk[u], off[u]);
-    ks[u] = vs[u] = 1.f;
-    if constexpr (F != kPlain) {
-      const long long sat = blk[u] * cv.ssb + h * cv.ssh + off[u];
-      ks[u] = cv.ks[sat];
-      vs[u] = cv.vs[sat];
-    }
-  }
-  Stored<ET, F> k[kRowsInFlight], v[kRowsInFlight];
-  const auto from = [&](int u) { return blk[u] * cv.sb + h * cv.sh + off[u] * cv.sn + 8 * c; };
+  const int end = min(n_end, T ? min(t_pitch, N) : N);
+  const int c = threadIdx.x & 15, j = n_begin + (int)blockIdx.x * kCacheTile + (int)(threadIdx.x >> 4);
+  if (j >= end) return;
+  const int n = T ? min(max(T[(size_t)row * t_pitch + j], 0), N - 1) : j;
+  int blk, off;
+  cache_place(cv.pm, b, n, blk, off);
+  const long long at = blk * cv.sb + h * cv.sh + off * cv.sn + 8 * c;
+  const long long sat = F == kPlain ? 0 : blk * cv.ssb + h * cv.ssh + off;
+  Stored<ET, F> k, v;
+  float ks = 1.f, vs = 1.f;
   if (K_out) {
-#pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) k[u] = load_stored<ET, F>((const RT*)cv.K + from(u));
+    k = load_stored<ET, F>((const RT*)cv.K + at);
+    if constexpr (F != kPlain) ks = cv.ks[sat];
   }
   if (V_out) {
-#pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) v[u] = load_stored<ET, F>((const RT*)cv.V + from(u));
+    v = load_stored<ET, F>((const RT*)cv.V + at);
+    if constexpr (F != kPlain) vs = cv.vs[sat];
   }
-  const long long to = ((long long)row * (n_end - n_begin) + (j0 - n_begin)) * kHeadDim + 8 * c;
-#pragma unroll
-  for (int u = 0; u < kRowsInFlight; ++u) {
-    if (j0 + 16 * u >= end) break;
-    if (K_out) store_vals<ET, F>(K_out + to + 16 * u * kHeadDim, k[u], ks[u]);
-    if (V_out) store_vals<ET, F>(V_out + to + 16 * u * kHeadDim, v[u], vs[u]);
-  }
+  const long long to = ((long long)row * (n_end - n_begin) + (j - n_begin)) * kHeadDim + 8 * c;
+  if (K_out) store_vals<ET, F>(K_out + to, k, ks);
+  if (V_out) store_vals<ET, F>(V_out + to, v, vs);
 }
 
 template <typename ET, CacheFmt F>
@@ -217,15 +211,15 @@ static hipError_t write_t(const fasa_shape& s, const CacheView& cv, const ChunkV
   const int hkv = s.n_kv_heads;
   const long long each = ((long long)ch.n_new * hkv + kCacheTile - 1) / kCacheTile;
   const long long tiles = chunk_tiles(ch.row_start != nullptr, s.batch, ch.n_new, ch.n_rows, hkv, kCacheTile);
-  return launch("fasa_cache_write", cache_write_kernel<ET, F>, dim3((unsigned)tiles), dim3(256), st, (const ET*)k_new, (const ET*)v_new, cv, ch,
-                s.batch, hkv, div_magic(hkv, (long long)ch.n_new * hkv), (int)each, kv_stride);
+  return launch("fasa_cache_write", cache_write_kernel<ET, F>, dim3((unsigned)tiles), dim3(256), st, (const ET*)k_new, (const ET*)v_new, cv, ch, s.batch,
+                hkv, div_magic(hkv, (long long)ch.n_new * hkv), (int)each, kv_stride);
 }
 template <typename ET, CacheFmt F>
 static hipError_t read_t(const fasa_shape& s, const CacheView& cv, const int32_t* T, const int32_t* n_ctx_seq, int n_begin, int n_end, void* K_out,
                          void* V_out, hipStream_t st) {
-  const int rows = s.batch * s.n_kv_heads, budget = s.budget < s.n_ctx ? s.budget : s.n_ctx;
-  return launch("fasa_cache_read", cache_read_kernel<ET, F>, dim3((n_end - n_begin + kCacheTile - 1) / kCacheTile, rows), dim3(256), st, (ET*)K_out,
-                (ET*)V_out, cv, T, budget, budget, n_ctx_seq, s.n_ctx, s.n_kv_heads, div_magic(s.n_kv_heads, rows), n_begin, n_end);
+  const int rows = s.batch * s.n_kv_heads, pitch = s.budget < s.n_ctx ? s.budget : s.n_ctx;
+  return launch("fasa_cache_read", cache_read_kernel<ET, F>, dim3((n_end - n_begin + kCacheTile - 1) / kCacheTile, rows), dim3(256), st, (ET*)K_out, (ET*)V_out,
+                cv, T, pitch, n_ctx_seq, s.n_ctx, s.n_kv_heads, div_magic(s.n_kv_heads, rows), n_begin, n_end);
 }
 
 #define FASA_BY_FORMAT(call, ...)                                                                                   \
