@@ -237,7 +237,7 @@ int fasa_decode_step_paged(const fasa_shape* shape, const fasa_paging* paging, c
  * 8-bit rows: one byte per value and one float32 scale per row (b, h, n), separately for K and V:
  *     scale = max |x| / Q, rounded to float32, Q = 127 (FASA_CACHE_INT8) or 448 (FASA_CACHE_E4M3);
  *     code  = the int8 (in [-127, 127]) or e4m3 (OCP 8-bit float: 4 exponent bits, 3 mantissa bits) number nearest to
- *             x / scale, ties to even; 0 where scale is 0.  (max |x| below 2^-120: code is clamped to +-Q.)
+ *             x / scale, ties to even, or +-Q where that is beyond Q (a tiny scale is rounded coarsely); 0 where scale is 0;
  * and the row stands for code * scale.  The quotient is rounded once, as if computed exactly, so codes do not depend on
  * how a kernel divides.  A row with an infinity or a NaN gets the scale NaN and codes 0.
  * Scales are laid out like the rows: scale of row (b, h, n) at b * scale_stride_b + h * scale_stride_h + n, or with
@@ -295,12 +295,14 @@ int fasa_cache_read(const fasa_shape* shape, const fasa_paging* paging, const fa
  * append): for token i of sequence b, p = N_b - n_b + i, query head hq, h = hq / G
  *     O[r,hq] = softmax_{n <= p}( q[r,hq] . K[b,h,n] / sqrt(d) ) V[b,h,n]
  * q and O of dtype, float32 accumulation and softmax; bf16: the weights of a softmax go into the product with V as bf16 numbers
- * (n_b * G > 16; up to that as two, 16 bits in all), O is rounded once.  8-bit rows enter as their codes, which bf16 holds
+ * (n_new * G > 16; up to that as two, 16 bits in all), O is rounded once.  8-bit rows enter as their codes, which bf16 holds
  * exactly, and scales stay float32.  n_new == 1 is full-KV decode attention over a paged or 8-bit cache.
  * Rows of O of no sequence are left as they were; rows of the cache at and beyond N_b and table entries beyond them have no effect,
  * whatever they hold.  O may not overlap q.  budget and n_fc are not used.
- * Needs a prepared workspace of fasa_chunk_workspace_bytes() (fasa_workspace_init, with any budget >= 1) and leaves it prepared; a
- * workspace large enough serves the decode steps of the same batch and head counts too. */
+ * Needs a prepared workspace of fasa_chunk_workspace_bytes() (fasa_workspace_init, with any budget >= 1) and leaves it prepared.  That size, of
+ * the largest chunk that a program makes, is enough for every chunk over any cache of the same batch and head counts with at most its n_new,
+ * rows (n_rows with row_start, batch * n_new without) and n_ctx; a workspace large enough serves the decode steps of the same batch and head
+ * counts too. */
 size_t fasa_chunk_workspace_bytes(const fasa_shape* shape, const fasa_chunk* chunk);
 int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const fasa_chunk* chunk,
                       const void* q, void* O, void* ws, size_t ws_bytes, void* stream);

@@ -9,6 +9,7 @@
 #include <cstdlib>
 #include <vector>
 
+#include "chunk_common.h"
 #include "fasa.h"
 #include "fasa_internal.h"
 #include "row_list.h"
@@ -217,6 +218,91 @@ int main() {
           while (bin > 0 && above + count[bin] < b) above += count[bin--];
           EXPECT(above + count[bin] >= b && count[bin] <= fasa::kHeldMany);
         }
+  }
+  // ---- chunks of new tokens: units cover every tile, partial results of any chunk fit the workspace of a larger one, tickets and LDS suffice ----
+  size_t chunks = 0;
+  for (int dtype : {FASA_BF16, FASA_F32})
+    for (int batch : {1, 2, 5, 64, 65, 512})
+      for (int hkv : {1, 3, 8, 100})
+        for (int g : {1, 4, 7, 8})
+          for (int n : {1, 64, 65, 1531, 32768, 1 << 20}) {
+            const fasa_shape s = shape(batch, hkv * g, hkv, 16, n, (n + 63) / 64 * 64, 1, dtype);
+            size_t last = 0;
+            for (int n_new : {1, 2, 4, 5, 16, 17, 32, 33, 129, 257, 2048, 40000}) {
+              if (n_new > n) continue;
+              for (bool packed : {false, true}) {
+                const int n_rows = packed ? batch * n_new : 0;
+                fasa::ChunkView ch{nullptr, nullptr, packed ? (const int32_t*)A : nullptr, n_new, n_rows, n};
+                const size_t parts = fasa::most_chunk_parts(s, ch);
+                EXPECT(parts >= last);
+                if (packed) last = parts;
+                fasa_chunk c{};
+                c.q_stride = c.o_stride = (int64_t)hkv * g * 128;
+                c.kv_stride = hkv * 128;
+                c.n_new = n_new;
+                c.n_rows = n_rows;
+                c.row_start = ch.row_start;
+                const size_t bytes = fasa_chunk_workspace_bytes(&s, &c);
+                if ((long long)n_rows * hkv * g > 0x7fffffffLL || (long long)batch * n_new * hkv * g > 8 * 0x7fffffffLL) {
+                  EXPECT(bytes == 0);                      // (refused)
+                  continue;
+                }
+                EXPECT(bytes % 256 == 0 && bytes >= fasa_workspace_bytes(&s) && bytes >= parts * (fasa::kChunkAccBytes + fasa::kChunkMlBytes));
+                for (int lesser : {n_new, (n_new + 1) / 2, 1})
+                  for (int shorter : {n, (n + 2) / 3})
+                    for (int rows_of : {n_rows, (n_rows + 2) / 3})
+                      for (bool ragged : {false, true})
+                        for (bool apart : {false, true}) {
+                          fasa_shape s1 = s;
+                          s1.n_ctx = std::max(shorter, lesser);
+                          const fasa::ChunkView of{nullptr, ragged ? (const int32_t*)A : nullptr, ch.row_start, lesser, rows_of, s1.n_ctx};
+                          const fasa::ChunkPlan p = fasa::plan_chunk(s1, apart, of);
+                          const long long tiles = fasa::chunk_tiles(packed, batch, lesser, rows_of, g, p.tile_rows);
+                          EXPECT(p.tile_rows >= 1 && p.tile_rows <= p.form.rows && (long long)p.per_seq * p.tile_rows >= (long long)lesser * g);
+                          EXPECT(p.part_acc_bytes <= parts * fasa::kChunkAccBytes && p.part_ml_bytes <= parts * fasa::kChunkMlBytes);
+                          EXPECT(p.units >= tiles && p.splits >= 1 && p.splits <= p.form.splits && (long long)p.units * hkv <= 0x7fffffffLL);
+                          const bool split = p.by_length || p.splits > 1;
+                          if (split) EXPECT(p.units * hkv <= std::max(p.form.resident, p.form.resident_by_length));
+                          if (p.by_length) EXPECT(batch <= 64 && tiles <= p.units);
+                          if (split) EXPECT(p.part_acc_bytes == (size_t)p.units * hkv * p.tile_rows * fasa::kChunkAccBytes);
+                          if (split && p.form.rows == fasa::kTokenForm.rows) EXPECT(8 * tiles <= fasa::kChunkTickets);
+                          EXPECT((p.by_length ? p.units : p.splits) * std::max(p.tile_rows < 17 ? p.tile_rows : 0, 8) * 4 <= 65536);
+                          ++chunks;
+                        }
+              }
+            }
+          }
+  EXPECT(chunks > 10000);
+  {
+    const fasa_shape s = shape(2, 8, 2, 16, 1000, 1024, 100);
+    fasa_cache plain{A, A, nullptr, nullptr, 0, 0, FASA_CACHE_PLAIN, 0}, bytes{A, A, (float*)A, (float*)A, 2048, 1024, FASA_CACHE_INT8, 0};
+    fasa_chunk c{nullptr, nullptr, nullptr, 1024, 256, 1024, 4, 0};
+    EXPECT(fasa_cache_write(&s, nullptr, nullptr, &c, A, A, nullptr) == FASA_EINVAL && fasa_cache_write(&s, nullptr, &plain, nullptr, A, A, nullptr) == FASA_EINVAL);
+    EXPECT(fasa_cache_write(nullptr, nullptr, &plain, &c, A, A, nullptr) == FASA_EINVAL && fasa_cache_write(&s, nullptr, &plain, &c, A, nullptr, nullptr) == FASA_EINVAL);
+    EXPECT(fasa_chunk_attend(&s, nullptr, &bytes, &c, A, A, nullptr, 1 << 30, nullptr) == FASA_EINVAL);
+    EXPECT(fasa_chunk_attend(&s, nullptr, &bytes, &c, A, A, A, 100, nullptr) == FASA_EWORKSPACE);
+    EXPECT(fasa_cache_read(&s, nullptr, &bytes, nullptr, nullptr, 0, 1001, A, A, nullptr) == FASA_EINVAL);
+    EXPECT(fasa_cache_read(&s, nullptr, &bytes, nullptr, nullptr, 7, 7, A, A, nullptr) == FASA_OK);
+    for (int wrong = 0; wrong < 12; ++wrong) {
+      fasa_cache k = bytes;
+      fasa_chunk h = c;
+      switch (wrong) {
+        case 0: k.K = nullptr; break;
+        case 1: k.v_scale = nullptr; break;
+        case 2: k.format = 3; break;
+        case 3: k.reserved = 1; break;
+        case 4: k.scale_stride_h = 1022; break;
+        case 5: k.K = (char*)A + 8; break;
+        case 6: h.n_new = 0; break;
+        case 7: h.n_new = 1001; break;
+        case 8: h.n_rows = 8; break;                       // (rows of a packed batch without their starts)
+        case 9: h.row_start = (const int32_t*)A; break;    // (the other way round)
+        case 10: h.n_ctx_seq = (const int32_t*)((char*)A + 2); break;
+        case 11: h.q_stride = h.kv_stride = 128; break;
+      }
+      EXPECT(fasa_chunk_attend(&s, nullptr, &k, &h, A, A, A, (size_t)1 << 40, nullptr) == FASA_EINVAL);
+      if (wrong != 11) EXPECT(fasa_cache_write(&s, nullptr, &k, &h, A, A, nullptr) == FASA_EINVAL);
+    }
   }
   // ---- bad shapes ----
   {

@@ -518,8 +518,7 @@ ChunkLayout chunk_layout(fasa_shape s, const ChunkView& ch, bool apart) {
   ChunkLayout L;
   L.plan = plan_chunk(s, apart, ch);
   s.budget = s.n_ctx;                     // (any: that part does not depend on it)
-  const WsLayout w = ws_layout(s);
-  L.acc_off = w.cand_off;
+  L.acc_off = ws_layout(s).cand_off;
   L.ml_off = align256(L.acc_off + L.plan.part_acc_bytes);
   L.total = align256(L.ml_off + L.plan.part_ml_bytes);
   return L;
@@ -559,8 +558,10 @@ int fasa_cache_read(const fasa_shape* shape, const fasa_paging* paging, const fa
 size_t fasa_chunk_workspace_bytes(const fasa_shape* shape, const fasa_chunk* chunk) {
   ChunkView ch;
   if (check_shape(shape, kNeedCtx | kNeedBudget) != FASA_OK || check_chunk(chunk, shape, 0, &ch) != FASA_OK) return 0;
-  // (of any cache; fasa_workspace_init asks for as much as the other calls need)
-  return std::max({chunk_layout(*shape, ch, false).total, chunk_layout(*shape, ch, true).total, ws_layout(*shape).total});
+  // (of any cache, and of the shorter chunks that a program serves with the same workspace; fasa_workspace_init asks for as much as the other calls need)
+  const WsLayout w = ws_layout(*shape);
+  const size_t parts = most_chunk_parts(*shape, ch);
+  return std::max(align256(align256(w.cand_off + parts * kChunkAccBytes) + parts * kChunkMlBytes), w.total);
 }
 
 int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const fasa_cache* cache, const fasa_chunk* chunk,
@@ -579,7 +580,7 @@ int fasa_chunk_attend(const fasa_shape* shape, const fasa_paging* paging, const 
   char* base = (char*)ws;
   const ChunkArgs a{cv, ch, (CacheFmt)cache->format, q, O, chunk->q_stride, chunk->o_stride, (float*)(base + L.acc_off),
                     (float*)(base + L.ml_off), (uint32_t*)base};
-  FASA_HIP(L.plan.wide ? launch_chunk_wide(*shape, L.plan, a, (hipStream_t)stream) : launch_chunk(*shape, L.plan, a, (hipStream_t)stream));
+  FASA_HIP(L.plan.form.rows == kTokenForm.rows ? launch_chunk(*shape, L.plan, a, (hipStream_t)stream) : launch_chunk_wide(*shape, L.plan, a, (hipStream_t)stream));
   return FASA_OK;
 }
 

@@ -13,14 +13,9 @@ namespace fasa {
 // do.  us, four / eight waves: bf16, 8 rows of 8192: 12.0 / 13.0, of 32768: 29.9 / 31.8, 128 of 4864 - 16384: 134 / 138; e4m3, 8 of 131072: 69.8 / 52.4 (with two tiles in
 // flight 58.0); float32, 37 new tokens over 4096: 18.2 / 15.9.
 template <typename ET, CacheFmt F> constexpr int kChunkWaves = F == kPlain && sizeof(ET) == 2 ? 4 : 8;
-constexpr int kChunkRows = 16;                           // query rows of a tile
-constexpr int kChunkLeast = 64;                          // tokens of a part, at least
-constexpr int kChunkSplits = 256;                        // parts of a tile, at most
-// Workgroups of a call whose tiles are split, at most; twice as many where sequences differ in length, whose shares may then be more alike (128 rows of 4864 - 16384,
-// int8: 89 / 86 us, e4m3 88 / 84).
-constexpr int kChunkResident = kAssumedCUs;
+constexpr int kChunkRows = kTokenForm.rows;
 constexpr int kTicketWords = 8;                          // from a tile's ticket to the next: tickets of different rows, whose workgroups run on different XCDs, share no line
-static_assert(2 * kChunkResident * kTicketWords <= kChunkTickets, "a ticket for each tile");
+static_assert(kTokenForm.resident_by_length * kTicketWords <= kChunkTickets, "a ticket for each tile");
 
 // One lane's share of 16 rows as stored; K: chunks hi, hi + 4, .. of 16 bytes of row lo, V: dims 8lo .. 8lo + 7 of rows 4hi .. 4hi + 3
 template <typename ET, CacheFmt F> struct RawKV {
@@ -82,7 +77,7 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
   // workgroups: heads fastest (the blocks of a paged cache often hold all heads' rows side by side)
   const int h = (int)(blockIdx.x % (unsigned)Hkv);
   ChunkUnit u;
-  if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, all_splits, units, kChunkLeast, blockIdx.x / (unsigned)Hkv, u)) return;
+  if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, all_splits, units, kTokenForm.least, blockIdx.x / (unsigned)Hkv, u)) return;
   const int b = u.b, splits = u.splits, qrow = u.tile * kChunkRows;
   const int rows = min(cap, u.seq.n_new * G - qrow);                 // of this tile
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -287,31 +282,43 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
     store_row(r, d4, make_float4(a.x * by, a.y * by, a.z * by, a.w * by));
   }
 }
-
-void plan_chunk_units(const fasa_shape& s, const ChunkView& ch, int rows, int resident, int resident_by_length, int least_share, int most_splits, ChunkPlan* p) {
-  const int G = s.n_q_heads / s.n_kv_heads;
-  const long long tiles = chunk_tiles(ch.row_start != nullptr, s.batch, ch.n_new, ch.n_rows, G, rows);
-  const long long units = resident / s.n_kv_heads, units_by_length = resident_by_length / s.n_kv_heads;
-  p->tile_rows = rows;
-  p->per_seq = (int)(((long long)ch.n_new * G + rows - 1) / rows);
-  p->by_length = (ch.n_ctx_seq || ch.n_new_seq) && s.batch > 1 && s.batch <= kWave && tiles <= units_by_length;
-  const long long most = (s.n_ctx + least_share - 1) / least_share;
-  const long long n = std::min({units / tiles, most, (long long)most_splits});
-  p->splits = n < 1 ? 1 : (int)n;
-  p->units = (int)(p->by_length ? std::min(units_by_length, tiles * most) : tiles * p->splits);
-  const size_t parts = p->splits == 1 && !p->by_length ? 0 : (size_t)p->units * s.n_kv_heads * rows;
-  p->part_acc_bytes = parts * kHeadDim * 4;
-  p->part_ml_bytes = parts * 8;
+// Few query rows, and float32: by 16-row tiles.  More: tiles of 256, and of 128 where a KV head has no more or where rows have to be looked up one by one.
+static ChunkForm chunk_form(const fasa_shape& s, bool apart, long long m) {
+  return s.dtype == FASA_F32 || m <= kTokenForm.rows ? kTokenForm : m <= kShortForm.rows || apart ? kShortForm : kDeepForm;
 }
 
-// Tiles of 16 query rows, or of all that there are.
 ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch) {
   const int G = s.n_q_heads / s.n_kv_heads;
-  if (s.dtype == FASA_BF16 && (long long)ch.n_new * G > kChunkRows) return plan_chunk_wide(s, apart, ch);
-  ChunkPlan p{};
   const long long m = (long long)ch.n_new * G;
-  plan_chunk_units(s, ch, m < kChunkRows ? (int)m : kChunkRows, kChunkResident, 2 * kChunkResident, kChunkLeast, kChunkSplits, &p);
+  ChunkPlan p{};
+  p.form = chunk_form(s, apart, m);
+  p.apart = apart;
+  p.tile_rows = p.form.rows == kTokenForm.rows && m < p.form.rows ? (int)m : p.form.rows;
+  p.per_seq = (int)((m + p.tile_rows - 1) / p.tile_rows);
+  const long long tiles = chunk_tiles(ch.row_start != nullptr, s.batch, ch.n_new, ch.n_rows, G, p.tile_rows);
+  const long long units = p.form.resident / s.n_kv_heads, units_by_length = p.form.resident_by_length / s.n_kv_heads;
+  p.by_length = (ch.n_ctx_seq || ch.n_new_seq) && s.batch > 1 && s.batch <= kWave && tiles <= units_by_length;
+  const long long most = (s.n_ctx + p.form.least - 1) / p.form.least;
+  const long long n = std::min({units / tiles, most, (long long)p.form.splits});
+  p.splits = n < 1 ? 1 : (int)n;
+  p.units = (int)(p.by_length ? std::min(units_by_length, tiles * most) : tiles * p.splits);
+  const size_t parts = p.splits == 1 && !p.by_length ? 0 : (size_t)p.units * s.n_kv_heads * p.tile_rows;
+  p.part_acc_bytes = parts * kChunkAccBytes;
+  p.part_ml_bytes = parts * kChunkMlBytes;
   return p;
+}
+
+// A call's tiles have `query` rows together at most and one unfinished tile for each sequence; parts are at most `most` to a tile, and as many as workgroups are resident.
+size_t most_chunk_parts(const fasa_shape& s, const ChunkView& ch) {
+  const long long G = s.n_q_heads / s.n_kv_heads, query = (ch.row_start ? (long long)ch.n_rows : (long long)s.batch * ch.n_new) * G;
+  size_t parts = 0;
+  for (const ChunkForm& f : {kTokenForm, kShortForm, kDeepForm}) {
+    if (f.rows != kTokenForm.rows && (s.dtype == FASA_F32 || ch.n_new * G <= kTokenForm.rows)) continue;
+    const long long most = (s.n_ctx + f.least - 1) / f.least;
+    const long long by_tokens = std::min(most, (long long)f.resident_by_length) * (query + (long long)s.batch * f.rows) * s.n_kv_heads;
+    parts = std::max(parts, (size_t)std::min(by_tokens, (long long)std::max(f.resident, f.resident_by_length) * f.rows));
+  }
+  return parts;
 }
 
 template <typename ET, CacheFmt F>

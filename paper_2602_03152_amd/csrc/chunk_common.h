@@ -167,25 +167,33 @@ hipError_t launch_cache_write(const fasa_shape& s, const CacheView& cv, CacheFmt
 hipError_t launch_cache_read(const fasa_shape& s, const CacheView& cv, CacheFmt fmt, const int32_t* T, const int32_t* n_ctx_seq,
                              int n_begin, int n_end, void* K_out, void* V_out, hipStream_t st);
 
-// How a chunk is attended.  wide: by chunk_wide.hip.
+// The forms of chunk attention, and what each divides a call into: tiles of `rows` query rows (new token, head of the group) of a sequence and KV head, whose tokens go to
+// parts of `least` or more, `splits` a tile at most, so that no more than `resident` workgroups run, `resident_by_length` where parts go by the sequences' lengths.
+struct ChunkForm {
+  int rows, resident, resident_by_length, least, splits;
+};
+constexpr ChunkForm kTokenForm{16, kAssumedCUs, 2 * kAssumedCUs, 64, 256};            // chunk.hip
+constexpr ChunkForm kShortForm{128, 2 * kAssumedCUs, 2 * kAssumedCUs, 256, 64};       // chunk_wide.hip
+constexpr ChunkForm kDeepForm{256, kAssumedCUs, kAssumedCUs, 256, 64};
+
 struct ChunkPlan {
-  bool wide;
-  bool apart;         // wide: rows are looked up one by one
+  ChunkForm form;
+  bool apart;         // rows are looked up one by one
   bool by_length;     // parts by the sequences' lengths
-  int tile_rows;      // query rows (new token, head of the group) of a tile
+  int tile_rows;      // query rows that a tile of this call has: form.rows, or all that there are
   int per_seq;        // query tiles of the longest sequence
   int splits;         // parts of a tile, where it is not by_length
   int units;          // workgroups of a KV head, at most
   size_t part_acc_bytes, part_ml_bytes;
 };
-// units, splits and partial results, for tiles of `rows` query rows: as many workgroups as are to be resident at once, of least_share tokens or more.
-void plan_chunk_units(const fasa_shape& s, const ChunkView& ch, int rows, int resident, int resident_by_length, int least_share, int most_splits, ChunkPlan* p);
 // apart: chunk_wide.hip has to look rows up one by one - pages of fewer tokens than a wave's load has rows, or strides beyond what it multiplies in 32 bits
 inline bool chunk_rows_apart(const CacheView& cv, CacheFmt fmt) {
   return (cv.pm.table != nullptr && ((1 << cv.pm.shift) < (fmt == kPlain ? 4 : 8) || cv.sb >= (1ll << 31))) || cv.sn >= (1ll << 27);
 }
 ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch);
-ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, const ChunkView& ch);
+// rows of partial results that no call with this one's batch and heads and at most its new tokens, rows and context goes beyond
+size_t most_chunk_parts(const fasa_shape& s, const ChunkView& ch);
+constexpr size_t kChunkAccBytes = kHeadDim * 4, kChunkMlBytes = 8;                    // of a row of partial results
 struct ChunkArgs {
   CacheView cv;
   ChunkView ch;

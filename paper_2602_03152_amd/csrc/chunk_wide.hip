@@ -30,7 +30,8 @@ __device__ __forceinline__ uint2 lds_read_tr(lds_ptr p) {
 }
 
 // What a workgroup works on: query rows [qt TR, qt TR + rows) of sequence b and KV head h, tokens [s0, s1).  part: where its partial result goes.
-constexpr int kWideLeast = 256;                           // tokens of a part, at least
+constexpr int kWideLeast = kShortForm.least;
+static_assert(kShortForm.least == kDeepForm.least);
 template <int TR> struct WideJob {
   int b, h, qt, splits, rows, row0, pos0, s0, s1, n_tiles;
   size_t part;
@@ -289,7 +290,8 @@ template <bool BYTES> struct WideQueries {
 };
 
 // Few query rows (up to 128 of a KV head): bound by reading the rows, which four waves share; two workgroups a compute unit have 64 KB of loads in flight.
-constexpr int kShortWaves = 4, kShortRows = 32 * kShortWaves;
+constexpr int kShortWaves = 4, kShortRows = kShortForm.rows;
+static_assert(kShortRows == 32 * kShortWaves);
 template <CacheFmt F, bool APART>
 __global__ __launch_bounds__(64 * kShortWaves, 2) void chunk_short_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
                                                                          uint16_t* __restrict__ O, float* __restrict__ part_acc,
@@ -357,7 +359,8 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void chunk_short_kernel(const 
 
 // Many: eight waves (256 rows a tile), two a SIMD.  In steps of 32 tokens: step u runs the logits of step u + 1 and the output of step u - 1 ahead of its own
 // softmax, so that the matrix cores have sixteen products in a row to do that wait for nothing.
-constexpr int kDeepWaves = 8, kDeepRows = 32 * kDeepWaves;
+constexpr int kDeepWaves = 8, kDeepRows = kDeepForm.rows;
+static_assert(kDeepRows == 32 * kDeepWaves);
 constexpr int kDeepSlots = 3;                             // tiles of K, and of V, in LDS: K of tiles T, T + 1 and V of T - 1, T are read while K of T + 2 and V of T + 1 are written
 template <CacheFmt F>
 __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
@@ -504,16 +507,6 @@ template <CacheFmt F> static hipError_t wide_f(const fasa_shape& s, const ChunkP
 }
 hipError_t launch_chunk_wide(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
   return a.fmt == kPlain ? wide_f<kPlain>(s, p, a, st) : a.fmt == kInt8 ? wide_f<kInt8>(s, p, a, st) : wide_f<kE4m3>(s, p, a, st);
-}
-
-// Tiles of 256 rows, of 128 where a KV head has no more or where rows have to be looked up one by one: two workgroups a compute unit then.
-ChunkPlan plan_chunk_wide(const fasa_shape& s, bool apart, const ChunkView& ch) {
-  ChunkPlan p{};
-  p.wide = true;
-  p.apart = apart;
-  const bool few = (long long)ch.n_new * (s.n_q_heads / s.n_kv_heads) <= kShortRows || apart;
-  plan_chunk_units(s, ch, few ? kShortRows : kDeepRows, few ? 2 * kAssumedCUs : kAssumedCUs, few ? 2 * kAssumedCUs : kAssumedCUs, kWideLeast, 64, &p);
-  return p;
 }
 
 }  // namespace fasa
