@@ -270,12 +270,21 @@ template <bool BYTES> struct WideQueries {
     if (job.splits == 1) {
       const float by = 1.0f / l;
       const int tok = job.token_of(my, G);
-      uint16_t* o = O + (long long)(job.row0 + tok) * o_stride + (long long)(job.h * G + (job.qt * TR + my) - tok * G) * D + 4 * half;
+      uint16_t* o = O + (long long)(job.row0 + tok) * o_stride + (long long)(job.h * G + (job.qt * TR + my) - tok * G) * D + 8 * half;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<uint2*>(o + 32 * d + 8 * g) = make_uint2(pack_bf16(oc[d][4 * g] * by, oc[d][4 * g + 1] * by), pack_bf16(oc[d][4 * g + 2] * by, oc[d][4 * g + 3] * by));
+        for (int g = 0; g < 4; g += 2) {                   // eight dims in a row to a lane: the lower half of the wave takes those of g, the upper of g + 1
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(oc[d][4 * g + 2 * i] * by, oc[d][4 * g + 2 * i + 1] * by),
+                                                            pack_bf16(oc[d][4 * g + 4 + 2 * i] * by, oc[d][4 * g + 5 + 2 * i] * by), false, false);
+            w[i] = x[0];
+            w[2 + i] = x[1];
+          }
+          *reinterpret_cast<uint4*>(o + 32 * d + 8 * g) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
       return;
     }
     const size_t to = job.part * TR + my;
