@@ -261,11 +261,10 @@ int main() {
                           EXPECT(p.tile_rows >= 1 && p.tile_rows <= p.form.rows && (long long)p.per_seq * p.tile_rows >= (long long)lesser * g);
                           EXPECT(p.part_acc_bytes <= parts * fasa::kChunkAccBytes && p.part_ml_bytes <= parts * fasa::kChunkMlBytes);
                           EXPECT(p.units >= tiles && p.splits >= 1 && p.splits <= p.form.splits && (long long)p.units * hkv <= 0x7fffffffLL);
-                          const bool split = p.by_length || p.splits > 1;
-                          if (split) EXPECT(p.units * hkv <= std::max(p.form.resident, p.form.resident_by_length));
-                          if (p.by_length) EXPECT(batch <= 64 && tiles <= p.units);
-                          if (split) EXPECT(p.part_acc_bytes == (size_t)p.units * hkv * p.tile_rows * fasa::kChunkAccBytes);
-                          if (split && p.form.rows == fasa::kTokenForm.rows) EXPECT(8 * tiles <= fasa::kChunkTickets);
+                          EXPECT(p.parts * hkv <= p.form.parts && p.part_acc_bytes == (size_t)p.parts * hkv * p.tile_rows * fasa::kChunkAccBytes);
+                          if (p.by_length) EXPECT(batch <= 64 && tiles <= p.units && p.parts == p.units && p.whole == 0);
+                          else EXPECT(p.parts == p.units - p.whole && p.units == p.whole + (tiles - p.whole) * p.splits && (p.parts > 0) == (p.splits > 1));
+                          if (p.form.rows == fasa::kTokenForm.rows && p.parts) EXPECT(p.whole == 0 && 8 * tiles <= fasa::kChunkTickets);
                           EXPECT((p.by_length ? p.units : p.splits) * std::max(p.tile_rows < 17 ? p.tile_rows : 0, 8) * 4 <= 65536);
                           ++chunks;
                         }

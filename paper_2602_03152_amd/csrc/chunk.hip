@@ -77,7 +77,7 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
   // workgroups: heads fastest (the blocks of a paged cache often hold all heads' rows side by side)
   const int h = (int)(blockIdx.x % (unsigned)Hkv);
   ChunkUnit u;
-  if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, all_splits, units, kTokenForm.least, blockIdx.x / (unsigned)Hkv, u)) return;
+  if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, 0, all_splits, units, kTokenForm.least, blockIdx.x / (unsigned)Hkv, u)) return;
   const int b = u.b, splits = u.splits, qrow = u.tile * kChunkRows;
   const int rows = min(cap, u.seq.n_new * G - qrow);                 // of this tile
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -298,11 +298,27 @@ ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch) {
   const long long tiles = chunk_tiles(ch.row_start != nullptr, s.batch, ch.n_new, ch.n_rows, G, p.tile_rows);
   const long long units = p.form.resident / s.n_kv_heads, units_by_length = p.form.resident_by_length / s.n_kv_heads;
   p.by_length = (ch.n_ctx_seq || ch.n_new_seq) && s.batch > 1 && s.batch <= kWave && tiles <= units_by_length;
-  const long long most = (s.n_ctx + p.form.least - 1) / p.form.least;
-  const long long n = std::min({units / tiles, most, (long long)p.form.splits});
-  p.splits = n < 1 ? 1 : (int)n;
-  p.units = (int)(p.by_length ? std::min(units_by_length, tiles * most) : tiles * p.splits);
-  const size_t parts = p.splits == 1 && !p.by_length ? 0 : (size_t)p.units * s.n_kv_heads * p.tile_rows;
+  const long long by_tokens = (s.n_ctx + p.form.least - 1) / p.form.least, most = std::min(by_tokens, (long long)p.form.splits);
+  p.splits = 1;
+  // Uniform: as many tiles whole as make full rounds, and the others in parts, so that their round is full too - or with tiles of 256 rows, which are bound by
+  // products, two rounds of smaller parts where that leaves less idle.  Costs in hundredths of what 64 tokens take: 5 for a workgroup's begin and end, 0.03 for a part to be
+  // written and joined.  us without / with, 32 heads over 8, 32768 tokens: 700 new ones (88 tiles
+  // for 256 workgroups) 499 / 445, 1100 (144) 953 / 702, 2200 (280) 1912 / 1200, 3000 (376) 1893 / 1578; over 4096: 700 82.6 / 82.8, 1100 127 / 110, 2200 159 / 148.
+  if (!p.by_length && units > 0) {
+    const long long left = p.form.rows == kDeepForm.rows ? tiles % units : tiles;     // tiles of the last round, which is not full
+    p.whole = (int)(tiles - left);
+    if (left) p.splits = (int)std::max(1ll, std::min(units / left, most));
+    if (left && p.form.rows == kDeepForm.rows) {
+      const long long seen = ((p.whole ? s.n_ctx - ch.n_new + left * p.form.rows / G : (long long)s.n_ctx) + 63) / 64, two = std::min(2 * units / left, most);
+      const auto cost = [&](long long n) { return ((left * n + units - 1) / units) * (100 * seen / n + 500) + (n > 1 ? 3 * left * n * s.n_kv_heads + 300 : 0); };
+      if (cost(two) < cost(p.splits)) p.splits = (int)two;
+      if (p.whole && cost(p.splits) >= cost(1)) p.splits = 1;
+    }
+  }
+  if (p.splits == 1 && !p.by_length) p.whole = (int)tiles;
+  p.units = (int)(p.by_length ? std::min(units_by_length, tiles * by_tokens) : p.whole + (tiles - p.whole) * p.splits);
+  p.parts = p.by_length ? p.units : p.units - p.whole;
+  const size_t parts = (size_t)p.parts * s.n_kv_heads * p.tile_rows;
   p.part_acc_bytes = parts * kChunkAccBytes;
   p.part_ml_bytes = parts * kChunkMlBytes;
   return p;
@@ -315,8 +331,8 @@ size_t most_chunk_parts(const fasa_shape& s, const ChunkView& ch) {
   for (const ChunkForm& f : {kTokenForm, kShortForm, kDeepForm}) {
     if (f.rows != kTokenForm.rows && (s.dtype == FASA_F32 || ch.n_new * G <= kTokenForm.rows)) continue;
     const long long most = (s.n_ctx + f.least - 1) / f.least;
-    const long long by_tokens = std::min(most, (long long)f.resident_by_length) * (query + (long long)s.batch * f.rows) * s.n_kv_heads;
-    parts = std::max(parts, (size_t)std::min(by_tokens, (long long)std::max(f.resident, f.resident_by_length) * f.rows));
+    const long long by_tokens = std::min(most, (long long)f.parts) * (query + (long long)s.batch * f.rows) * s.n_kv_heads;
+    parts = std::max(parts, (size_t)std::min(by_tokens, (long long)f.parts * f.rows));
   }
   return parts;
 }

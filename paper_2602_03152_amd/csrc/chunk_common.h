@@ -79,23 +79,25 @@ __device__ __forceinline__ bool find_chunk_tile(const ChunkView& c, int batch, i
   }
   return false;
 }
-// A workgroup's part of the work: tokens [split * share, ..) of a query tile of a sequence.  first: the unit of the tile's split 0.
+// A workgroup's part of the work: tokens [split * share, ..) of a query tile of a sequence.  first: the place of the tile's split 0 among the partial results.
 struct ChunkUnit {
   SeqChunk seq;
   int b, tile, split, splits, first;
   int share;                    // 0: the tile's tokens in equal parts
 };
-// Unit y of the grid.  Uniform: every tile in `splits` parts.  By length (units != 0; up to 64 sequences): a batch of mixed lengths would wait for its longest
+// Unit y of the grid.  Uniform: the first `whole` tiles are a unit each, every other one is in `splits` parts.  By length (units != 0; up to 64 sequences): a batch of mixed lengths would wait for its longest
 // sequence, so all parts are of about as many tokens, and a sequence has as many of them as it takes: the smallest share (a multiple of 64 tokens, of
 // least_share or more) with which all the tiles' parts are no more than the units.  Every wave finds it by itself, a lane a sequence.
 template <int TILE>
-__device__ __forceinline__ bool find_chunk_unit(const ChunkView& c, int batch, int G, int tiles_each, int splits, int units, int least_share, unsigned y, ChunkUnit& u) {
+__device__ __forceinline__ bool find_chunk_unit(const ChunkView& c, int batch, int G, int tiles_each, int whole, int splits, int units, int least_share, unsigned y, ChunkUnit& u) {
   if (units == 0) {
-    u.split = (int)(y % (unsigned)splits);
-    u.splits = splits;
-    u.first = (int)y - u.split;
+    const bool one = y < (unsigned)whole;
+    const unsigned part = one ? 0u : y - (unsigned)whole, id = one ? y : (unsigned)whole + part / (unsigned)splits;
+    u.splits = one ? 1 : splits;
+    u.split = one ? 0 : (int)(part % (unsigned)splits);
+    u.first = (int)part - u.split;
     u.share = 0;
-    if (!find_chunk_tile<TILE>(c, batch, G, tiles_each, y / (unsigned)splits, u.b, u.tile)) return false;
+    if (!find_chunk_tile<TILE>(c, batch, G, tiles_each, id, u.b, u.tile)) return false;
     u.seq = seq_chunk(c, u.b);
     return u.tile < (int)(((long long)u.seq.n_new * G + TILE - 1) / TILE);
   }
@@ -169,12 +171,13 @@ hipError_t launch_cache_read(const fasa_shape& s, const CacheView& cv, CacheFmt 
 
 // The forms of chunk attention, and what each divides a call into: tiles of `rows` query rows (new token, head of the group) of a sequence and KV head, whose tokens go to
 // parts of `least` or more, `splits` a tile at most, so that no more than `resident` workgroups run, `resident_by_length` where parts go by the sequences' lengths.
+// No more than `parts` workgroups of a call have partial results.
 struct ChunkForm {
-  int rows, resident, resident_by_length, least, splits;
+  int rows, resident, resident_by_length, least, splits, parts;
 };
-constexpr ChunkForm kTokenForm{16, kAssumedCUs, 2 * kAssumedCUs, 64, 256};            // chunk.hip
-constexpr ChunkForm kShortForm{128, 2 * kAssumedCUs, 2 * kAssumedCUs, 256, 64};       // chunk_wide.hip
-constexpr ChunkForm kDeepForm{256, kAssumedCUs, kAssumedCUs, 256, 64};
+constexpr ChunkForm kTokenForm{16, kAssumedCUs, 2 * kAssumedCUs, 64, 256, 2 * kAssumedCUs};            // chunk.hip
+constexpr ChunkForm kShortForm{128, 2 * kAssumedCUs, 2 * kAssumedCUs, 256, 64, 2 * kAssumedCUs};       // chunk_wide.hip
+constexpr ChunkForm kDeepForm{256, kAssumedCUs, kAssumedCUs, 256, 64, 2 * kAssumedCUs};
 
 struct ChunkPlan {
   ChunkForm form;
@@ -182,8 +185,10 @@ struct ChunkPlan {
   bool by_length;     // parts by the sequences' lengths
   int tile_rows;      // query rows that a tile of this call has: form.rows, or all that there are
   int per_seq;        // query tiles of the longest sequence
-  int splits;         // parts of a tile, where it is not by_length
+  int whole;          // tiles before those that are split (0: by_length)
+  int splits;         // parts of a tile behind, where it is not by_length
   int units;          // workgroups of a KV head, at most
+  int parts;          // of them with partial results: all behind `whole`, where there are any
   size_t part_acc_bytes, part_ml_bytes;
 };
 // apart: chunk_wide.hip has to look rows up one by one - pages of fewer tokens than a wave's load has rows, or strides beyond what it multiplies in 32 bits

@@ -37,10 +37,10 @@ template <int TR> struct WideJob {
   size_t part;
   __device__ __forceinline__ int token_of(int r, int G) const { return (qt * TR + r) / G; }      // new token of the tile's row r
   // False: nothing to do.  Workgroups: heads fastest (those of a sequence read the same blocks, and a head's lie on one XCD where there are eight).
-  __device__ __forceinline__ bool find(const ChunkView& ch, int batch, int Hkv, int G, int tiles_each, int all_splits, int units, int all_units) {
+  __device__ __forceinline__ bool find(const ChunkView& ch, int batch, int Hkv, int G, int tiles_each, int whole, int all_splits, int units, int all_parts) {
     h = (int)(blockIdx.x % (unsigned)Hkv);
     ChunkUnit u;
-    if (!find_chunk_unit<TR>(ch, batch, G, tiles_each, all_splits, units, kWideLeast, blockIdx.x / (unsigned)Hkv, u)) return false;
+    if (!find_chunk_unit<TR>(ch, batch, G, tiles_each, whole, all_splits, units, kWideLeast, blockIdx.x / (unsigned)Hkv, u)) return false;
     b = u.b;
     splits = u.splits;
     const int m = u.seq.n_new * G;
@@ -53,7 +53,7 @@ template <int TR> struct WideJob {
     s0 = (int)min((long long)u.split * share, (long long)seen);
     s1 = min(seen, s0 + share);
     n_tiles = (s1 - s0 + kWideTok - 1) / kWideTok;
-    part = (size_t)h * all_units + u.first + u.split;
+    part = (size_t)h * all_parts + u.first + u.split;
     return true;
   }
 };
@@ -305,13 +305,13 @@ template <CacheFmt F, bool APART>
 __global__ __launch_bounds__(64 * kShortWaves, 2) void chunk_short_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
                                                                          uint16_t* __restrict__ O, float* __restrict__ part_acc,
                                                                          float2* __restrict__ part_ml, CacheView cv, ChunkView ch, int batch, int Hkv,
-                                                                         int G, int tiles_each, int splits, int units, int all_units, long long q_stride, long long o_stride,
+                                                                         int G, int tiles_each, int whole, int splits, int units, int all_parts, long long q_stride, long long o_stride,
                                                                          float scale_log2e) {
   constexpr bool BYTES = F != kPlain;
   extern __shared__ __align__(16) unsigned char smem[];    // [2][K tile, V tile], then scales [2][k 64, v 64]
   float* const sm_scale = reinterpret_cast<float*>(smem + 4 * kTileBytes);
   WideJob<kShortRows> job;
-  if (!job.find(ch, batch, Hkv, G, tiles_each, splits, units, all_units)) return;
+  if (!job.find(ch, batch, Hkv, G, tiles_each, whole, splits, units, all_parts)) return;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   using Loader = WideLoader<F, kShortWaves, APART>;
   const Loader ld(cv, K, V, q, job.b, job.h, job.s1, wave, lane);
@@ -375,7 +375,7 @@ template <CacheFmt F>
 __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const uint16_t* __restrict__ q, const void* __restrict__ K, const void* __restrict__ V,
                                                                        uint16_t* __restrict__ O, float* __restrict__ part_acc,
                                                                        float2* __restrict__ part_ml, CacheView cv, ChunkView ch, int batch, int Hkv,
-                                                                       int G, int tiles_each, int splits, int units, int all_units, long long q_stride, long long o_stride,
+                                                                       int G, int tiles_each, int whole, int splits, int units, int all_parts, long long q_stride, long long o_stride,
                                                                        float scale_log2e) {
   constexpr int NT = 64 * kDeepWaves, B = kTileBytes;
   constexpr bool BYTES = F != kPlain;
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
   float* const ssk = reinterpret_cast<float*>(smem + 2 * kDeepSlots * B);
   float* const ssv = ssk + kDeepSlots * kWideTok;
   WideJob<kDeepRows> job;
-  if (!job.find(ch, batch, Hkv, G, tiles_each, splits, units, all_units)) return;
+  if (!job.find(ch, batch, Hkv, G, tiles_each, whole, splits, units, all_parts)) return;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   using Loader = WideLoader<F, kDeepWaves, false>;
   using Rows = typename Loader::Rows;
@@ -455,16 +455,16 @@ __global__ __launch_bounds__(64 * kDeepWaves, 2) void chunk_deep_kernel(const ui
 template <int TR> constexpr int kMergeWgs = TR / 64;
 template <int TR>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restrict__ part_acc, const float2* __restrict__ part_ml, uint16_t* __restrict__ O,
-                                                          ChunkView ch, int batch, int Hkv, int G, int tiles_each, int all_splits, int units, int all_units,
+                                                          ChunkView ch, int batch, int Hkv, int G, int tiles_each, int whole, int all_splits, int units, int all_parts,
                                                           long long o_stride) {
   extern __shared__ float weights[];                                   // [8][parts]
   const int h = (int)(blockIdx.x % (unsigned)Hkv);
   ChunkUnit u;
-  if (!find_chunk_unit<TR>(ch, batch, G, tiles_each, all_splits, units, kWideLeast, blockIdx.x / (unsigned)Hkv, u) || u.splits == 1) return;
+  if (!find_chunk_unit<TR>(ch, batch, G, tiles_each, whole, all_splits, units, kWideLeast, (unsigned)whole + blockIdx.x / (unsigned)Hkv, u) || u.splits == 1) return;
   const int wgs = u.splits * kMergeWgs<TR>, wg = u.split * kMergeWgs<TR> + (int)blockIdx.y;
   const int n = u.splits, m = u.seq.n_new * G, qt = (m + TR - 1) / TR - 1 - u.tile, rows = min(TR, m - qt * TR);
   const int group = threadIdx.x >> 5, c = threadIdx.x & 31;
-  const size_t part0 = ((size_t)h * all_units + u.first) * TR;
+  const size_t part0 = ((size_t)h * all_parts + u.first) * TR;
   float* const w = weights + group * n;
   const int per = (rows + wgs - 1) / wgs, r1 = min(rows, (wg + 1) * per);
   for (int r = wg * per + group; r < r1; r += 8) {
@@ -504,10 +504,10 @@ static hipError_t wide_t(Kernel kernel, size_t lds, const fasa_shape& s, const C
   const int hkv = s.n_kv_heads, G = s.n_q_heads / hkv, units = p.by_length ? p.units : 0;
   const hipError_t e = launch_lds("fasa_chunk_attend", kernel, dim3((unsigned)p.units * (unsigned)hkv), dim3(2 * TR), lds, st, (const uint16_t*)a.q,
                                   (const void*)a.cv.K, (const void*)a.cv.V, (uint16_t*)a.O, a.part_acc, (float2*)a.part_ml, a.cv, a.ch, s.batch, hkv, G,
-                                  p.per_seq, p.splits, units, p.units, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
-  if (e != hipSuccess || (p.splits == 1 && !p.by_length)) return e;
-  return launch_lds("fasa_chunk_merge", chunk_merge_kernel<TR>, dim3((unsigned)p.units * (unsigned)hkv, kMergeWgs<TR>), dim3(256), (p.by_length ? p.units : p.splits) * 8 * sizeof(float),
-                    st, (const float*)a.part_acc, (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.splits, units, p.units, a.o_stride);
+                                  p.per_seq, p.whole, p.splits, units, p.parts, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
+  if (e != hipSuccess || p.parts == 0) return e;
+  return launch_lds("fasa_chunk_merge", chunk_merge_kernel<TR>, dim3((unsigned)p.parts * (unsigned)hkv, kMergeWgs<TR>), dim3(256), (p.by_length ? p.units : p.splits) * 8 * sizeof(float),
+                    st, (const float*)a.part_acc, (const float2*)a.part_ml, (uint16_t*)a.O, a.ch, s.batch, hkv, G, p.per_seq, p.whole, p.splits, units, p.parts, a.o_stride);
 }
 template <CacheFmt F> static hipError_t wide_f(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {
   const size_t scales = F == kPlain ? 0 : kWideTok * 4;
