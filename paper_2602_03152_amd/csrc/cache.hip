@@ -46,8 +46,6 @@ template <CacheFmt F> __device__ __forceinline__ uint32_t codes_of(const float* 
     return __builtin_amdgcn_perm(cd, ab, 0x05040100u);
   }
 }
-// The values that four codes stand for.
-template <CacheFmt F> __device__ __forceinline__ f32x4_t values_of(uint32_t w) { return bytes_to_f32<F>(w); }
 
 // A row's eight values of this lane -> codes, and the row's scale.  codes: the nearest to x / s, decided as if the quotient were exact.  A product with 1 / s is off
 // by less than 2^-22 of itself, which matters only within that of a tie: where the codes of 2^-21 less and 2^-21 more differ (a lane in 10^3 for int8, in 10^4 for e4m3) the
@@ -92,7 +90,7 @@ template <typename ET, CacheFmt F> __device__ __forceinline__ uint2 quantise_row
       const uint2 e = make_uint2(codes_of<F>(hi), codes_of<F>(hi + 4));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const f32x4_t vl = values_of<F>(h ? c.y : c.x), vh = values_of<F>(h ? e.y : e.x);
+        const f32x4_t vl = bytes_to_f32<F>(h ? c.y : c.x), vh = bytes_to_f32<F>(h ? e.y : e.x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float mid = 0.5f * (vl[i] + vh[i]), over = fmaf(-mid, s, f[4 * h + i]);

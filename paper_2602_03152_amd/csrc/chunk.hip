@@ -282,16 +282,25 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
     store_row(r, d4, make_float4(a.x * by, a.y * by, a.z * by, a.w * by));
   }
 }
-// Few query rows, and float32: by 16-row tiles.  More: tiles of 256, and of 128 where a KV head has no more or where rows have to be looked up one by one.
-static ChunkForm chunk_form(const fasa_shape& s, bool apart, long long m) {
-  return s.dtype == FASA_F32 || m <= kTokenForm.rows ? kTokenForm : m <= kShortForm.rows || apart ? kShortForm : kDeepForm;
+// Float32, and up to 16 query rows of a KV head: by 16-row tiles (20 rows, 32768 tokens: those 36.9 us, chunk_wide.hip 36.4; 8-bit 31.1 / 30.2).  Up to 128, or where rows
+// have to be looked up one by one: the short form (32 heads over 8, 32768 tokens, 32 new ones: 50.4 us, the deep form 58.0; 33: 59.5 / 58.0, 64: 70 / 65).  That one also where
+// tiles of 256 rows in the least parts would leave half of the compute units without work (us, short / deep: 512 tokens, 256 new ones 20.6 / 25.7; 2048, 128: 21.7 / 26.3;
+// 4096, 64: 21.6 / 26.1; and with twice as many parts 2048, 256: 31.5 / 31.1, 8192, 64: 31.6 / 30.8), and for contexts of up to 1024 tokens, of which a workgroup has so few that its
+// begin and end count, which two on a compute unit hide (prompts, 4 of 1024: 63 / 73, 8 of 512: 43 / 50, 4 of 2048: 195 / 189).
+static ChunkForm chunk_form(const fasa_shape& s, bool apart, const ChunkView& ch) {
+  const int G = s.n_q_heads / s.n_kv_heads;
+  const long long m = (long long)ch.n_new * G;
+  if (s.dtype == FASA_F32 || m <= kTokenForm.rows) return kTokenForm;
+  if (m <= kShortForm.rows || apart || s.n_ctx <= 1024) return kShortForm;
+  const long long tiles = chunk_tiles(ch.row_start != nullptr, s.batch, ch.n_new, ch.n_rows, G, kDeepForm.rows);
+  return tiles * s.n_kv_heads * ((s.n_ctx + kDeepForm.least - 1) / kDeepForm.least) <= kDeepForm.resident / 2 ? kShortForm : kDeepForm;
 }
 
 ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch) {
   const int G = s.n_q_heads / s.n_kv_heads;
   const long long m = (long long)ch.n_new * G;
   ChunkPlan p{};
-  p.form = chunk_form(s, apart, m);
+  p.form = chunk_form(s, apart, ch);
   p.apart = apart;
   p.tile_rows = p.form.rows == kTokenForm.rows && m < p.form.rows ? (int)m : p.form.rows;
   p.per_seq = (int)((m + p.tile_rows - 1) / p.tile_rows);

@@ -124,13 +124,13 @@ def test_rows_that_overlap_leave_the_workspace_prepared():
         check(t)
 
 
-def _many_heads(fmt, dtype, batch, hkv, G, N, lens, paged, n):
+def _many_heads(fmt, dtype, batch, hkv, G, N, lens, paged, n, page=16):
     hq = hkv * G
     byte = fmt != "plain"
     pool = [torch.zeros(batch, hkv, N, D, dtype=torch.uint8 if byte else DT[dtype], device="cuda") for _ in range(2)]
     pitch = (N + 3) // 4 * 4
     scale = [torch.zeros(batch, hkv, pitch, device="cuda") if byte else None for _ in range(2)]
-    page, paging = 16, None
+    paging = None
     shape = fb.make_shape(batch, hq, hkv, D, 16, N, (N + 63) // 64 * 64, 1, dtype, kv_stride_b=hkv * N * D, kv_stride_h=N * D, kv_stride_n=D)
     if paged:                             # the same rows as blocks [block][page][head]
         blocks = batch * ((N + page - 1) // page)
@@ -181,3 +181,11 @@ def test_parts_of_many_tiles(fmt, dtype, batch, hkv, N, paged, n):
 def test_full_rounds_and_parts(fmt, paged, hkv, G, n, N, batch):
     """More 256-row tiles than workgroups run at once, or almost as many: whole ones, then parts."""
     _many_heads(fmt, "bf16", batch, hkv, G, N, [N] * batch, paged, n)
+
+
+@pytest.mark.parametrize("fmt,page", [("plain", 0), ("plain", 4), ("int8", 8), ("e4m3", 32), ("int8", 0)])
+@pytest.mark.parametrize("G,n", [(1, 129), (1, 300), (3, 43), (7, 37), (7, 74), (8, 33), (4, 129)])
+@pytest.mark.parametrize("lens", [[1025], [1087], [1531, 700], [1600, 300, 1100, 1025]])
+def test_256_row_tiles_at_odd_sizes(fmt, page, G, n, lens):
+    """The kernel of many query rows where tiles, tokens and blocks end anywhere; sequences of unequal lengths, one as long as its new tokens."""
+    _many_heads(fmt, "bf16", len(lens), 66, G, max(lens), [max(m, n) for m in lens], page > 0, n, max(page, 1))
