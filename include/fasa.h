@@ -298,7 +298,8 @@ int fasa_cache_read(const fasa_shape* shape, const fasa_paging* paging, const fa
  * (n_new * G > 16; up to that as two, 16 bits in all), O is rounded once.  8-bit rows enter as their codes, which bf16 holds
  * exactly, and scales stay float32.  n_new == 1 is full-KV decode attention over a paged or 8-bit cache.
  * Rows of O of no sequence are left as they were; rows of the cache at and beyond N_b and table entries beyond them have no effect,
- * whatever they hold.  O may not overlap q.  budget and n_fc are not used.
+ * whatever they hold.  A row of K, or an 8-bit row, that is not finite reaches the results of the tokens that see it, and of no others; values of an
+ * FASA_CACHE_PLAIN row of V have to be finite (the tokens of the chunk before it weigh it with 0).  O may not overlap q.  budget and n_fc are not used.
  * Needs a prepared workspace of fasa_chunk_workspace_bytes() (fasa_workspace_init, with any budget >= 1) and leaves it prepared.  That size, of
  * the largest chunk that a program makes, is enough for every chunk over any cache of the same batch and head counts with at most its n_new,
  * rows (n_rows with row_start, batch * n_new without) and n_ctx; a workspace large enough serves the decode steps of the same batch and head

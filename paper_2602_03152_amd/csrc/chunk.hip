@@ -186,9 +186,9 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
         TileKV<ET> kv;
         const f32x4_t k_by = ks;
         f32x4_t v_by;
-        // (scales behind the split's end were not this tile's and may be anything)
+        // (scales of tokens that the query does not see may be anything, a NaN too)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v_by[e] = j0 + 4 * hi + e < s1 ? vs[e] : 0.f;
+        for (int e = 0; e < 4; ++e) v_by[e] = j0 + 4 * hi + e < my_end ? vs[e] : 0.f;
         raw.k_to(kv);
         raw.v_to(kv);
         load_k();

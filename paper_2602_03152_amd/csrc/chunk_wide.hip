@@ -247,6 +247,10 @@ template <bool BYTES> struct WideQueries {
       for (int i = 0; i < 16; ++i) sum[i & 1] += sv[i];
       l_run += sum[0] + sum[1];
       by_scale(sv, vs);
+      if (n0 + 32 > all) {                                 // (a scale may be a NaN)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sv[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < my_end ? sv[i] : 0.f;
+      }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) p.w[i] = pack_bf16(sv[2 * i], sv[2 * i + 1]);

@@ -145,6 +145,31 @@ def test_large_logits(fmt, n):
     check(t)
 
 
+NOT_FINITE = [("bf16", "plain", 2, 4, 70), ("bf16", "int8", 2, 4, 70), ("f32", "e4m3", 2, 20, 70), ("f32", "plain", 2, 20, 70), ("bf16", "plain", 2, 40, 333),
+              ("bf16", "int8", 2, 40, 333), ("bf16", "e4m3", 40, 70, 1100), ("bf16", "plain", 40, 70, 1100)]
+
+
+@pytest.mark.parametrize("dtype,fmt,hkv,n,N,which", [(*case, w) for case in NOT_FINITE for w in (["K"] if case[1] == "plain" else ["K", "V", "both"])])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_token_that_is_not_finite_reaches_no_earlier_one(dtype, fmt, hkv, n, N, which, bad):
+    """The chunk's last but two token has a row of NaN or infinities: tokens before it are as without, those from it on are NaN.  (Plain rows of V have to be finite.)"""
+    t = build([N], [n], 4 * hkv, hkv, fmt, dtype, seed=n, page=16)
+    k, v = (draw_rows(np.random.default_rng(n), (n, hkv, D), dtype).cuda() for _ in range(2))
+    fb.fasa_cache_write(t["shape"], t["cache"].paging, t["cache"].cache, t["chunk"], k, v)
+    call(t)
+    good = t["O"].clone()
+    if which != "V":
+        k[n - 3] = bad
+    if which != "K":
+        v[n - 3] = bad
+    fb.fasa_cache_write(t["shape"], t["cache"].paging, t["cache"].cache, t["chunk"], k, v)
+    call(t)
+    torch.cuda.synchronize()
+    first = t["c"].start[0]
+    assert torch.equal(t["O"][first:first + n - 3], good[first:first + n - 3])
+    assert not torch.isfinite(t["O"][first + n - 3:first + n].float()).any()
+
+
 def test_equal_keys_give_the_mean():
     t = build([129], [17], 4, 1, seed=1)
     t["cache"].K.fill_(0.5)
