@@ -501,8 +501,8 @@ int check_chunk(const fasa_chunk* c, const fasa_shape* s, unsigned rows, ChunkVi
   const int64_t q_row = (int64_t)s->n_q_heads * s->head_dim, kv_row = (int64_t)s->n_kv_heads * s->head_dim;
   if ((rows & kOfNew) && (c->kv_stride < kv_row || c->kv_stride % 8 != 0)) return FASA_EINVAL;
   if ((rows & kOfQuery) && (c->q_stride < q_row || c->q_stride % 8 != 0 || c->o_stride < q_row || c->o_stride % 8 != 0)) return FASA_EINVAL;
-  // the kernels count rows times heads of a sequence, rows of the batch, and workgroups in 31 bits
-  if ((long long)c->n_new * s->n_q_heads > 0x7fffffffLL || (long long)s->batch * c->n_new > 0x7fffffffLL ||
+  // the kernels count rows times heads of a sequence, rows of the batch, workgroups, and tokens some tiles behind the last in 31 bits
+  if (s->n_ctx > 0x7fff0000 || (long long)c->n_new * s->n_q_heads > 0x7fffffffLL || (long long)s->batch * c->n_new > 0x7fffffffLL ||
       (long long)c->n_rows * s->n_q_heads > 0x7fffffffLL || (long long)s->batch * c->n_new * s->n_q_heads > 8 * 0x7fffffffLL)
     return FASA_EUNSUPPORTED;
   *out = ChunkView{c->n_new_seq, c->n_ctx_seq, c->row_start, c->n_new, c->n_rows, s->n_ctx};

@@ -152,6 +152,13 @@ def test_workspace():
     assert attend(_shape(budget=0), None, cache(), chunk()) == EWS             # the budget is not used
 
 
+def test_lengths_that_31_bits_do_not_hold():
+    s = _shape(n_ctx=0x7fff0001, n_cap=0x7fffffc0)
+    assert attend(s, None, cache(), chunk()) == EUNSUP and write(s, None, cache(), chunk()) == EUNSUP
+    assert fb.fasa_chunk_workspace_bytes(s, chunk()) == 0
+    assert attend(_shape(n_ctx=0x7fff0000, n_cap=0x7fffffc0), None, cache(), chunk()) == EWS
+
+
 def test_binding_raises_and_checks_structures():
     s = _shape()
     with pytest.raises(fb.FasaError) as e:

@@ -189,3 +189,24 @@ def test_full_rounds_and_parts(fmt, paged, hkv, G, n, N, batch):
 def test_256_row_tiles_at_odd_sizes(fmt, page, G, n, lens):
     """The kernel of many query rows where tiles, tokens and blocks end anywhere; sequences of unequal lengths, one as long as its new tokens."""
     _many_heads(fmt, "bf16", len(lens), 66, G, max(lens), [max(m, n) for m in lens], page > 0, n, max(page, 1))
+
+
+@pytest.mark.parametrize("n,page", [(40, 16), (40, 4), (20, 16), (20, 1)])
+def test_many_rows_captured(n, page):
+    """Parts and their merge in one graph, replayed as lengths change, with the program's own calls in between."""
+    from tests.test_gpu_chunk_attend import build, call
+    t = build([1100, 900], [n, n], 80, 20, "plain", page=page, seed=n, n_ctx=1200)
+    lens = t["c"].n_ctx_seq
+    call(t)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(t)
+    for a, b in ((1100, 900), (61, 333), (1090, 25), (700, 899), (1100, 900)):
+        lens.copy_(torch.tensor([a, b], dtype=torch.int32))
+        t["base"].fill_(77.0)
+        call(t)
+        eager = t["O"].clone()
+        t["base"].fill_(77.0)
+        g.replay()
+        assert torch.equal(t["O"], eager), (a, b)
