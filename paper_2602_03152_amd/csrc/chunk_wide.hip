@@ -7,8 +7,9 @@
 //   O^T += V^T P^T (dims x queries): what the lane has of P^T, as bf16, is the second operand as it stands: its k-slots 0-3, 4-7 are the tokens of registers
 //                 8 s .. 8 s + 7 of k-step s.  V^T with tokens in that order comes out of LDS by transposing reads (ds_read_b64_tr_b16: 16 lanes get
 //                 one column each of four rows).  A new maximum rescales a lane's own accumulators.
-// LDS rows are 256 bytes of 16-byte chunks; chunk c of token t is stored at c ^ (t mod 16) (K) or c ^ 2 (t mod 8) (V), so that the lanes
-// of a read fall on all banks.  8-bit rows become bf16 (exactly) on their way into LDS, once for all waves; their scales multiply logits and weights in float32.
+// LDS rows are 256 bytes of 16-byte chunks; chunk c of token t is stored at c ^ (t mod 16) (K) or c ^ 4 (t mod 4) ^ (t / 4 mod 2) (V), so that the lanes that
+// are served at once fall on all banks: 16 lanes of a read of K, 32 of a transposing one (four rows, 64 bytes each).  8-bit rows become bf16 (exactly) on their way into
+// LDS, once for all waves; their scales multiply logits and weights in float32.
 #include "chunk_common.h"
 
 namespace fasa {
@@ -21,7 +22,7 @@ constexpr int kWideTok = 64;                              // tokens of a tile
 constexpr int kTileBytes = kWideTok * kHeadDim * 2;       // of K or V in LDS
 
 __device__ __forceinline__ int swz_k(int t) { return t & 15; }
-__device__ __forceinline__ int swz_v(int t) { return 2 * (t & 7); }
+__device__ __forceinline__ int swz_v(int t) { return (4 * (t & 3)) ^ ((t >> 2) & 1); }
 
 // Four bf16 of one column of V for each of 16 lanes, out of four rows of LDS
 __device__ __forceinline__ uint2 lds_read_tr(lds_ptr p) {
