@@ -78,7 +78,7 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
   const int h = (int)(blockIdx.x % (unsigned)Hkv);
   ChunkUnit u;
   if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, 0, all_splits, units, kTokenForm.least, blockIdx.x / (unsigned)Hkv, u)) return;
-  const int b = u.b, splits = u.splits, qrow = u.tile * kChunkRows;
+  const int b = u.b, splits = u.splits, qrow = ((u.seq.n_new * G - 1) / kChunkRows - u.tile) * kChunkRows;     // the longest first
   const int rows = min(cap, u.seq.n_new * G - qrow);                 // of this tile
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int lo = lane & 15, hi = lane >> 4;
@@ -305,7 +305,12 @@ ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch) {
   p.tile_rows = p.form.rows == kTokenForm.rows && m < p.form.rows ? (int)m : p.form.rows;
   p.per_seq = (int)((m + p.tile_rows - 1) / p.tile_rows);
   const long long tiles = chunk_tiles(ch.row_start != nullptr, s.batch, ch.n_new, ch.n_rows, G, p.tile_rows);
-  const long long units = p.form.resident / s.n_kv_heads, units_by_length = p.form.resident_by_length / s.n_kv_heads;
+  const long long units = p.form.resident / s.n_kv_heads;
+  // By length: parts of a sequence are whole, so its last is half a part too long on average, tiles / 2 of them in all; with twice the workgroups half of that, but then a
+  // compute unit has two after each other, which costs about what 800 tokens take.  (us, once / twice, 8 KV heads, int8: 4 sequences of 670 - 1531 9.7 / 15.2, 8 of 2816 - 8192
+  // 25.1 / 31.7, 16 of 2432 - 8192 49.0 / 50.7, 4 of 28672 - 65536 86.7 / 91.2, 16 of 4864 - 16384 88.6 / 84.6, bf16 138.6 / 139.1.)
+  const bool once = tiles <= units && (long long)s.batch * s.n_ctx * tiles < 3200 * units * units;
+  const long long units_by_length = once ? units : p.form.resident_by_length / s.n_kv_heads;
   p.by_length = (ch.n_ctx_seq || ch.n_new_seq) && s.batch > 1 && s.batch <= kWave && tiles <= units_by_length;
   const long long by_tokens = (s.n_ctx + p.form.least - 1) / p.form.least, most = std::min(by_tokens, (long long)p.form.splits);
   p.splits = 1;
