@@ -264,7 +264,7 @@ int main() {
                           EXPECT(p.parts * hkv <= p.form.parts && p.part_acc_bytes == (size_t)p.parts * hkv * p.tile_rows * fasa::kChunkAccBytes);
                           if (p.by_length) EXPECT(batch <= 64 && tiles <= p.units && p.parts == p.units && p.whole == 0);
                           else EXPECT(p.parts == p.units - p.whole && p.units == p.whole + (tiles - p.whole) * p.splits && (p.parts > 0) == (p.splits > 1));
-                          if (p.form.rows == fasa::kTokenForm.rows && p.parts) EXPECT(p.whole == 0 && 8 * tiles <= fasa::kChunkTickets);
+                          if (p.form.rows == fasa::kTokenForm.rows && p.parts) EXPECT(8 * (tiles - p.whole) <= fasa::kChunkTickets);
                           EXPECT((p.by_length ? p.units : p.splits) * std::max(p.tile_rows < 17 ? p.tile_rows : 0, 8) * 4 <= 65536);
                           ++chunks;
                         }

@@ -15,7 +15,7 @@ namespace fasa {
 template <typename ET, CacheFmt F> constexpr int kChunkWaves = F == kPlain && sizeof(ET) == 2 ? 4 : 8;
 constexpr int kChunkRows = kTokenForm.rows;
 constexpr int kTicketWords = 8;                          // from a tile's ticket to the next: tickets of different rows, whose workgroups run on different XCDs, share no line
-static_assert(kTokenForm.resident_by_length * kTicketWords <= kChunkTickets, "a ticket for each tile");
+static_assert(kTokenForm.resident <= kTokenForm.resident_by_length && kTokenForm.resident_by_length * kTicketWords <= kChunkTickets, "a ticket for each tile that is split");
 
 // One lane's share of 16 rows as stored; K: chunks hi, hi + 4, .. of 16 bytes of row lo, V: dims 8lo .. 8lo + 7 of rows 4hi .. 4hi + 3
 template <typename ET, CacheFmt F> struct RawKV {
@@ -64,7 +64,7 @@ template <typename ET, CacheFmt F, bool SMALL>
 __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
     const ET* __restrict__ q, const typename RowType<ET, F>::type* __restrict__ K, const typename RowType<ET, F>::type* __restrict__ V, ET* __restrict__ O,
     float* __restrict__ part_acc, float2* __restrict__ part_ml, uint32_t* __restrict__ tickets, CacheView cv, ChunkView ch, int batch, int Hkv, int G,
-    int tiles_each, int all_splits, int units, int all_units, int cap, long long q_stride, long long o_stride, float scale_log2e) {
+    int tiles_each, int whole, int all_splits, int units, int all_parts, int cap, long long q_stride, long long o_stride, float scale_log2e) {
   constexpr int D = kHeadDim, NWV = kChunkWaves<ET, F>, NT = 64 * NWV, ROUND = 16 * NWV;     // tokens of a round of the waves
   constexpr bool F32 = sizeof(ET) == 4;
   using RT = typename RowType<ET, F>::type;
@@ -77,7 +77,7 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
   // workgroups: heads fastest (the blocks of a paged cache often hold all heads' rows side by side)
   const int h = (int)(blockIdx.x % (unsigned)Hkv);
   ChunkUnit u;
-  if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, 0, all_splits, units, kTokenForm.least, blockIdx.x / (unsigned)Hkv, u)) return;
+  if (!find_chunk_unit<kChunkRows>(ch, batch, G, tiles_each, whole, all_splits, units, kTokenForm.least, blockIdx.x / (unsigned)Hkv, u)) return;
   const int b = u.b, splits = u.splits, qrow = ((u.seq.n_new * G - 1) / kChunkRows - u.tile) * kChunkRows;     // the longest first
   const int rows = min(cap, u.seq.n_new * G - qrow);                 // of this tile
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -214,7 +214,7 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
     else *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w));
   };
   // partial results: [head][unit][cap]
-  const size_t part0 = ((size_t)h * all_units + u.first) * cap;
+  const size_t part0 = ((size_t)h * all_parts + u.first) * cap;
   float* pa = part_acc + part0 * D;
   float2* pm = part_ml + part0;
   for (int x = t; x < rows * (D / 4); x += NT) {
@@ -241,7 +241,7 @@ __global__ __launch_bounds__((64 * kChunkWaves<ET, F>), 2) void chunk_kernel(
   }
   if (splits == 1) return;
   publish_barrier();
-  uint32_t* tk = tickets + (size_t)(b * Hkv + h) * kChunkTickets + kTicketWords * u.tile;
+  uint32_t* tk = tickets + (size_t)(b * Hkv + h) * kChunkTickets + kTicketWords * u.slot;
   if (t == 0) ticket = atomicAdd(tk, 1u);
   __syncthreads();
   if (ticket != (uint32_t)splits - 1u) return;
@@ -314,20 +314,17 @@ ChunkPlan plan_chunk(const fasa_shape& s, bool apart, const ChunkView& ch) {
   p.by_length = (ch.n_ctx_seq || ch.n_new_seq) && s.batch > 1 && s.batch <= kWave && tiles <= units_by_length;
   const long long by_tokens = (s.n_ctx + p.form.least - 1) / p.form.least, most = std::min(by_tokens, (long long)p.form.splits);
   p.splits = 1;
-  // Uniform: as many tiles whole as make full rounds, and the others in parts, so that their round is full too - or with tiles of 256 rows, which are bound by
-  // products, two rounds of smaller parts where that leaves less idle.  Costs in hundredths of what 64 tokens take: 5 for a workgroup's begin and end, 0.03 for a part to be
-  // written and joined.  us without / with, 32 heads over 8, 32768 tokens: 700 new ones (88 tiles
-  // for 256 workgroups) 499 / 445, 1100 (144) 953 / 702, 2200 (280) 1912 / 1200, 3000 (376) 1893 / 1578; over 4096: 700 82.6 / 82.8, 1100 127 / 110, 2200 159 / 148.
+  // Uniform: as many tiles whole as make full rounds, and the others in parts, so many that what they take in rounds of workgroups is the least.
+  // us without / with: 32 heads over 8, 32768 tokens: 700 new ones (88 tiles for 256 workgroups) 499 / 445, 1100 (144) 953 / 702, 2200 (280) 1912 / 1200, 3000 (376) 1893 / 1578; over
+  // 4096: 700 82.6 / 82.8, 1100 127 / 110, 2200 159 / 148.  A token each, int8 and bf16, 8 KV heads, of 12000: 20 sequences 137 / 108, 198 / 185, 12: 74.7 / 70.1, 114 / 114; of 4000: 20:
+  // 49.8 / 44.1, 69 / 67, 36: 96 / 69, 152 / 110, 5: 14.3 / 14.4, 17.1 / 17.2.  72 x 8 drafted ones 279 / 230.  Float32, 150 new ones over 4096: 174 / 113.
   if (!p.by_length && units > 0) {
-    const long long left = p.form.rows == kDeepForm.rows ? tiles % units : tiles;     // tiles of the last round, which is not full
+    const long long left = tiles % units, all = p.form.parts / s.n_kv_heads;
     p.whole = (int)(tiles - left);
-    if (left) p.splits = (int)std::max(1ll, std::min(units / left, most));
-    if (left && p.form.rows == kDeepForm.rows) {
-      const long long seen = ((p.whole ? s.n_ctx - ch.n_new + left * p.form.rows / G : (long long)s.n_ctx) + 63) / 64, two = std::min(2 * units / left, most);
-      const auto cost = [&](long long n) { return ((left * n + units - 1) / units) * (100 * seen / n + 500) + (n > 1 ? 3 * left * n * s.n_kv_heads + 300 : 0); };
-      if (cost(two) < cost(p.splits)) p.splits = (int)two;
-      if (p.whole && cost(p.splits) >= cost(1)) p.splits = 1;
-    }
+    const long long seen = p.whole && s.batch == 1 ? s.n_ctx - ch.n_new + left * p.tile_rows / G : s.n_ctx;      // (of one sequence the shortest tiles are left)
+    const auto cost = [&](long long n) { return (left * n + units - 1) / units * (seen / n + p.form.begin) + (n > 1 ? left * n * s.n_kv_heads * p.form.join + 40 : 0); };
+    for (long long n = 2; n <= most && left * n <= all; ++n)
+      if (cost(n) < cost(p.splits)) p.splits = (int)n;
   }
   if (p.splits == 1 && !p.by_length) p.whole = (int)tiles;
   p.units = (int)(p.by_length ? std::min(units_by_length, tiles * by_tokens) : p.whole + (tiles - p.whole) * p.splits);
@@ -360,7 +357,7 @@ static hipError_t chunk_t(const fasa_shape& s, const ChunkPlan& p, const ChunkAr
   const auto kernel = small ? chunk_kernel<ET, F, true> : chunk_kernel<ET, F, false>;
   return launch_lds("fasa_chunk_attend", kernel, dim3((unsigned)p.units * (unsigned)hkv), dim3(64 * kChunkWaves<ET, F>), totals > merge ? totals : merge, st,
                     (const ET*)a.q, (const RT*)a.cv.K, (const RT*)a.cv.V, (ET*)a.O, a.part_acc, (float2*)a.part_ml, a.tickets, a.cv, a.ch, s.batch, hkv, G,
-                    p.per_seq, p.splits, p.by_length ? p.units : 0, p.units, p.tile_rows, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
+                    p.per_seq, p.whole, p.splits, p.by_length ? p.units : 0, p.parts, p.tile_rows, a.q_stride, a.o_stride, 1.4426950408889634f / sqrtf((float)s.head_dim));
 }
 
 hipError_t launch_chunk(const fasa_shape& s, const ChunkPlan& p, const ChunkArgs& a, hipStream_t st) {

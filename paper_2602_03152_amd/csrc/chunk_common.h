@@ -84,6 +84,7 @@ struct ChunkUnit {
   SeqChunk seq;
   int b, tile, split, splits, first;
   int share;                    // 0: the tile's tokens in equal parts
+  int slot;                     // of the tile among a row's (sequence's and KV head's) that are split: below the workgroups of a KV head
 };
 // Unit y of the grid.  Uniform: the first `whole` tiles are a unit each, every other one is in `splits` parts.  By length (units != 0; up to 64 sequences): a batch of mixed lengths would wait for its longest
 // sequence, so all parts are of about as many tokens, and a sequence has as many of them as it takes: the smallest share (a multiple of 64 tokens, of
@@ -97,6 +98,7 @@ __device__ __forceinline__ bool find_chunk_unit(const ChunkView& c, int batch, i
     u.split = one ? 0 : (int)(part % (unsigned)splits);
     u.first = (int)part - u.split;
     u.share = 0;
+    u.slot = (int)(part / (unsigned)splits);
     if (!find_chunk_tile<TILE>(c, batch, G, tiles_each, id, u.b, u.tile)) return false;
     u.seq = seq_chunk(c, u.b);
     return u.tile < (int)(((long long)u.seq.n_new * G + TILE - 1) / TILE);
@@ -129,6 +131,7 @@ __device__ __forceinline__ bool find_chunk_unit(const ChunkView& c, int batch, i
   u.split = local - u.tile * u.splits;
   u.first = (int)y - u.split;
   u.share = 64 * hi;
+  u.slot = u.tile;
   u.seq = SeqChunk{__builtin_amdgcn_readlane(s.n_ctx, u.b), __builtin_amdgcn_readlane(s.n_new, u.b), __builtin_amdgcn_readlane(s.row, u.b)};
   return true;
 }
@@ -170,14 +173,14 @@ hipError_t launch_cache_read(const fasa_shape& s, const CacheView& cv, CacheFmt 
                              int n_begin, int n_end, void* K_out, void* V_out, hipStream_t st);
 
 // The forms of chunk attention, and what each divides a call into: tiles of `rows` query rows (new token, head of the group) of a sequence and KV head, whose tokens go to
-// parts of `least` or more, `splits` a tile at most, so that no more than `resident` workgroups run, `resident_by_length` where parts go by the sequences' lengths.
-// No more than `parts` workgroups of a call have partial results.
+// parts of `least` or more, `splits` a tile at most, for rounds of `resident` workgroups, `resident_by_length` where parts go by the sequences' lengths.  No more than `parts`
+// workgroups of a call have partial results.  What a workgroup's begin and end cost beside its tokens, and what a part costs to be joined, in tokens of a tile: begin, join.
 struct ChunkForm {
-  int rows, resident, resident_by_length, least, splits, parts;
+  int rows, resident, resident_by_length, least, splits, parts, begin, join;
 };
-constexpr ChunkForm kTokenForm{16, kAssumedCUs, 2 * kAssumedCUs, 64, 256, 2 * kAssumedCUs};            // chunk.hip
-constexpr ChunkForm kShortForm{128, 2 * kAssumedCUs, 2 * kAssumedCUs, 256, 64, 2 * kAssumedCUs};       // chunk_wide.hip
-constexpr ChunkForm kDeepForm{256, kAssumedCUs, kAssumedCUs, 256, 64, 2 * kAssumedCUs};
+constexpr ChunkForm kTokenForm{16, kAssumedCUs, 2 * kAssumedCUs, 64, 256, 4 * kAssumedCUs, 800, 0};            // chunk.hip
+constexpr ChunkForm kShortForm{128, 2 * kAssumedCUs, 2 * kAssumedCUs, 256, 64, 2 * kAssumedCUs, 500, 1};       // chunk_wide.hip
+constexpr ChunkForm kDeepForm{256, kAssumedCUs, kAssumedCUs, 256, 64, 2 * kAssumedCUs, 320, 2};
 
 struct ChunkPlan {
   ChunkForm form;

@@ -210,3 +210,10 @@ def test_many_rows_captured(n, page):
         t["base"].fill_(77.0)
         g.replay()
         assert torch.equal(t["O"], eager), (a, b)
+
+
+@pytest.mark.parametrize("fmt,paged", [("plain", True), ("int8", False), ("e4m3", True)])
+@pytest.mark.parametrize("dtype,hkv,G,n,N,batch", [("f32", 64, 1, 70, 900, 1), ("f32", 64, 4, 33, 1200, 2), ("f32", 1, 1, 4800, 5000, 1), ("bf16", 64, 4, 4, 3000, 5),
+                                                   ("bf16", 100, 8, 1, 2500, 3)])
+def test_full_rounds_and_parts_of_16_row_tiles(dtype, hkv, G, n, N, batch, fmt, paged):
+    _many_heads(fmt, dtype, batch, hkv, G, N, [N] * batch, paged, n)
