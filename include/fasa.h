@@ -300,6 +300,7 @@ int fasa_cache_read(const fasa_shape* shape, const fasa_paging* paging, const fa
  * Rows of O of no sequence are left as they were; rows of the cache at and beyond N_b and table entries beyond them have no effect,
  * whatever they hold.  A row of K, or an 8-bit row, that is not finite reaches the results of the tokens that see it, and of no others; values of an
  * FASA_CACHE_PLAIN row of V have to be finite (the tokens of the chunk before it weigh it with 0).  O may not overlap q.  budget and n_fc are not used.
+ * n_ctx up to 2^31 - 2^16; n_new * n_q_heads, batch * n_new and n_rows * n_q_heads below 2^31 (else FASA_EUNSUPPORTED).
  * Needs a prepared workspace of fasa_chunk_workspace_bytes() (fasa_workspace_init, with any budget >= 1) and leaves it prepared.  That size, of
  * the largest chunk that a program makes, is enough for every chunk over any cache of the same batch and head counts with at most its n_new,
  * rows (n_rows with row_start, batch * n_new without) and n_ctx; a workspace large enough serves the decode steps of the same batch and head
